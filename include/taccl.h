@@ -331,6 +331,218 @@ taccl_status_t taccl_connections_batch(taccl_plan_t plan, int64_t n, const uint8
 taccl_status_t taccl_generate_host(taccl_plan_t plan, uint64_t seed, int64_t first, int64_t count,
                                    uint8_t *routes, uint32_t *prio);
 
+/* ------------------------------------------------------------------------
+ * Expert layer around an Alltoall: what makes the chunks that an Alltoall
+ * plan moves, and what takes them back.
+ *
+ * With E experts spread evenly over P ranks, rank s writes its token rows
+ * into a buffer [E][capacity][cols]: the rows of the experts of rank d are
+ * contiguous, so they are the chunks (s, d, 0 .. chunks_per_rank-1) of
+ * TACCL_ALLTOALL, of E/P * capacity * (bytes of a row) / chunks_per_rank
+ * bytes each. taccl_norm gives the rows (also in 8 bits, half the chunk),
+ * taccl_route the expert and the place of every row and the loss that keeps
+ * the experts' loads, and so the chunks, even; taccl_dispatch fills the
+ * buffer, taccl_combine reads the rows that come back. The *_backward calls
+ * are the gradients; the gradient of taccl_dispatch is taccl_combine without
+ * weights.
+ *
+ * Conventions: arrays are device memory of the caller, the last axis is
+ * contiguous and strides (in elements) are those of the rows. Any alignment
+ * of the element's size will do; rows that start on 16 bytes are fastest.
+ * The work runs asynchronously on `stream` of the current device, nothing is
+ * allocated, and the same inputs give the same bits. Statistics, sums and
+ * products are held in 32-bit floats and rounded once, to the output's type
+ * (to nearest even). Errors (synchronous): INVALID_ARGUMENT for null
+ * pointers, negative sizes, strides below the row's length, misaligned
+ * pointers or unknown types, LIMIT for sizes beyond the stated ones, HIP if
+ * a launch fails.
+ * ------------------------------------------------------------------------ */
+typedef enum { TACCL_F32 = 0, TACCL_BF16 = 1, TACCL_F16 = 2 } taccl_dtype_t;
+
+/*
+ * Root-mean-square norm of rows after the residual's addition:
+ *   h = x + residual, y = weight * h / sqrt(mean(h^2) + eps),
+ * with y from the unrounded h. Per row any of
+ *   out: y; total: h (the next layer's residual; may be `residual` or `x`
+ *     itself, with the same stride); q, scale: y in 8 bits (OCP e4m3) with one
+ *     scale per `group` columns (32, 64, 128 or 256; 0: one per row),
+ *     scale = max(max |y| of the group, 2^-100) / 448 and q = y / scale to
+ *     nearest even; a NaN or infinite y is NaN in q and a NaN leaves its
+ *     group's scale alone. scale has ceil(cols / group) values per row.
+ * 1 <= cols <= 16384, rows <= 2^21. rows == 0 is a no-op.
+ */
+typedef struct {
+  int64_t rows;
+  int32_t cols;
+  int32_t dtype; /* taccl_dtype_t of x, residual, weight, out, total */
+  float eps;     /* >= 0 */
+  int32_t group;
+  const void *x, *residual; /* residual: or NULL */
+  int64_t x_stride, residual_stride;
+  const void *weight;  /* [cols] */
+  void *out, *total;   /* each: or NULL */
+  int64_t out_stride, total_stride;
+  uint8_t *q;          /* or NULL; scale then too */
+  float *scale;
+  int64_t q_stride, scale_stride;
+} taccl_norm_t;
+taccl_status_t taccl_norm(const taccl_norm_t *a, taccl_stream_t stream);
+
+/*
+ * Gradient of y (above) with respect to h, which x and residual share, and
+ * to the weight, for h as given (the stored total):
+ *   r = 1 / sqrt(mean(h^2) + eps), a = weight * dout,
+ *   dx = dtotal + r * a - h * r^3 * mean(a * h),  dweight = sum over rows of
+ *   dout * h * r (32-bit floats; zero without rows).
+ * dx may be dout, dtotal or h itself, with the same stride. `workspace`:
+ * taccl_norm_workspace(cols) bytes, 4-byte aligned, not shared with another
+ * call in flight.
+ */
+typedef struct {
+  int64_t rows;
+  int32_t cols;
+  int32_t dtype; /* of dout, h, dtotal, weight, dx */
+  float eps;
+  const void *dout, *h, *dtotal; /* dtotal: gradient that reaches h another way, or NULL */
+  int64_t dout_stride, h_stride, dtotal_stride;
+  const void *weight;
+  void *dx;
+  int64_t dx_stride;
+  float *dweight;
+  void *workspace;
+  int64_t workspace_bytes;
+} taccl_norm_backward_t;
+taccl_status_t taccl_norm_backward(const taccl_norm_backward_t *a, taccl_stream_t stream);
+/* 4096 * cols (0 for cols < 1) */
+int64_t taccl_norm_workspace(int32_t cols);
+
+/*
+ * Choice of k experts per token from the router's logits, their places, the
+ * experts' loads and the balance loss:
+ *   p = softmax(logits) of a token; the k largest logits are chosen, equal
+ *   ones in the order of their index, a logit of minus infinity never and a
+ *   NaN never (it makes the token's p NaN);
+ *   experts[t][j], weights[t][j]: the j-th choice and its p (renorm: divided
+ *     by the sum over the token's choices); -1 and 0 where there is none;
+ *   slots[t][j]: the number of earlier tokens that chose the same expert, -1
+ *     from `capacity` on (0: no limit);
+ *   counts[e]: tokens that chose e, also those past the capacity;
+ *   prob_sums[e]: sum over tokens of p_e; rows: tokens with a choice to make;
+ *   loss = coef * E * sum_e counts[e] / (rows * k) * prob_sums[e] / rows, the
+ *     balance loss (0 without rows).
+ * Tokens with mask 0, and tokens whose logits are all minus infinity, choose
+ * nothing and count nowhere; nothing of a masked token's logits is used.
+ * 1 <= E <= 1024, 1 <= k <= min(E, 16), tokens <= 2^21.
+ * `workspace`: taccl_route_workspace(E) bytes, 4-byte aligned, not shared
+ * with another call in flight.
+ */
+typedef struct {
+  int64_t tokens;
+  int32_t num_experts, k;
+  int32_t dtype; /* of logits */
+  int32_t renorm;
+  float coef;
+  int64_t capacity;
+  const void *logits;
+  int64_t logits_stride;
+  const uint8_t *mask; /* [tokens], or NULL */
+  int32_t *experts;    /* [tokens][k] */
+  float *weights;      /* [tokens][k] */
+  int32_t *slots;      /* [tokens][k] */
+  int32_t *counts;     /* [E] */
+  float *prob_sums;    /* [E] */
+  float *loss;         /* [1] */
+  int32_t *rows;       /* [1] */
+  void *workspace;
+  int64_t workspace_bytes;
+} taccl_route_t;
+taccl_status_t taccl_route(const taccl_route_t *a, taccl_stream_t stream);
+int64_t taccl_route_workspace(int32_t num_experts);
+
+/*
+ * Gradient of the loss (times *dloss) and of the weights (with dweights
+ * [tokens][k]) with respect to the logits, the choices held fixed. counts and
+ * rows may be sums over several ranks' tokens: the gradient is then that of
+ * the loss of all of them, with prob_sums summed over the ranks too. Zero for
+ * tokens that chose nothing.
+ */
+typedef struct {
+  int64_t tokens;
+  int32_t num_experts, k;
+  int32_t dtype; /* of logits and dlogits */
+  int32_t renorm;
+  float coef;
+  const void *logits;
+  int64_t logits_stride;
+  const uint8_t *mask;
+  const int32_t *experts;
+  const int32_t *counts;
+  const int32_t *rows;
+  const float *dweights; /* or NULL */
+  const float *dloss;    /* [1], or NULL */
+  void *dlogits;
+  int64_t dlogits_stride;
+} taccl_route_backward_t;
+taccl_status_t taccl_route_backward(const taccl_route_backward_t *a, taccl_stream_t stream);
+
+/*
+ * Buffer of rows by expert, for the three calls below: out, buffer and
+ * dbuffer are [E][capacity][cols], contiguous. Choice j of token t has the
+ * row (experts[t][j], slots[t][j]); a choice whose expert or slot lies outside
+ * the buffer has none. 1 <= E <= 1024, 1 <= k <= 16, 1 <= capacity < 2^31,
+ * tokens <= 2^21, 1 <= cols <= 2^20. Offsets in the buffer are 64-bit.
+ *
+ * Dispatch: out[row of (t, j)] = x[t], and rows from counts[e] on are zero.
+ * Elements of 1, 2 or 4 bytes; with the scales of 8-bit rows, scale
+ * [tokens][scale_cols] goes to out_scale [E][capacity][scale_cols] alike.
+ */
+typedef struct {
+  int64_t tokens, capacity;
+  int32_t num_experts, k, cols;
+  int32_t element_bytes; /* 1, 2 or 4 */
+  int32_t scale_cols;    /* 0 without scales */
+  const void *x;
+  int64_t x_stride;
+  const float *scale;
+  int64_t scale_stride;
+  const int32_t *experts, *slots; /* [tokens][k] */
+  const int32_t *counts;          /* [E] */
+  void *out;
+  float *out_scale;
+} taccl_dispatch_t;
+taccl_status_t taccl_dispatch(const taccl_dispatch_t *a, taccl_stream_t stream);
+
+/* Combine: out[t] = sum over the choices j of t that have a row, in order, of
+ * weights[t][j] * buffer[row] (weights NULL: 1). */
+typedef struct {
+  int64_t tokens, capacity;
+  int32_t num_experts, k, cols;
+  int32_t dtype; /* of buffer and out */
+  const void *buffer;
+  const int32_t *experts, *slots;
+  const float *weights; /* [tokens][k], or NULL */
+  void *out;
+  int64_t out_stride;
+} taccl_combine_t;
+taccl_status_t taccl_combine(const taccl_combine_t *a, taccl_stream_t stream);
+
+/* Its gradient: dbuffer[row of (t, j)] = weights[t][j] * dout[t], zero in rows
+ * from counts[e] on; dweights[t][j] = sum over columns of dout[t] *
+ * buffer[row], 0 without a row. */
+typedef struct {
+  int64_t tokens, capacity;
+  int32_t num_experts, k, cols;
+  int32_t dtype; /* of dout, buffer and dbuffer */
+  const void *dout;
+  int64_t dout_stride;
+  const void *buffer;
+  const int32_t *experts, *slots, *counts;
+  const float *weights; /* [tokens][k] */
+  void *dbuffer;
+  float *dweights; /* [tokens][k] */
+} taccl_combine_backward_t;
+taccl_status_t taccl_combine_backward(const taccl_combine_backward_t *a, taccl_stream_t stream);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char *taccl_last_error(void);
 

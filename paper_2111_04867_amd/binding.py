@@ -50,6 +50,9 @@ EXPORTS = ["taccl_topology_create", "taccl_topology_destroy", "taccl_collective_
            "taccl_plan_route_options",
            "taccl_plan_path", "taccl_plan_link_costs", "taccl_plan_upload", "taccl_eval_batch",
            "taccl_connections_batch", "taccl_generate_host", "taccl_count_faults",
+           "taccl_norm", "taccl_norm_backward", "taccl_norm_workspace", "taccl_route",
+           "taccl_route_backward", "taccl_route_workspace", "taccl_dispatch", "taccl_combine",
+           "taccl_combine_backward",
            "taccl_last_error",
            "taccl_version"]
 

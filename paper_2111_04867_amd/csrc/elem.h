@@ -1,0 +1,99 @@
+// Rows of 16-byte vectors and wavefront reductions of the expert-layer
+// kernels (gfx950).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "wave.h"
+
+namespace taccl {
+
+using bf16_t = __bf16;
+using f16_t = _Float16;
+
+// VE elements of one 16-byte vector; the global access needs only the
+// element's alignment (gfx950 takes any address).
+template <class T>
+struct Vec {
+  static constexpr int kN = 16 / (int)sizeof(T);
+  typedef T V __attribute__((ext_vector_type(16 / sizeof(T))));
+  typedef V U __attribute__((aligned(sizeof(T))));
+};
+
+// The vector at p. Of the columns from `left` on nothing is read or written
+// and they come as zero; kTail: fewer than kN may be left (else none or kN).
+template <class T, bool kTail>
+__device__ __forceinline__ typename Vec<T>::V load_vec(const T *p, int left) {
+  constexpr int N = Vec<T>::kN;
+  typename Vec<T>::V v;
+  if (left >= N) {
+    v = *(const typename Vec<T>::U *)p;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i++) v[i] = kTail && i < left ? p[i] : (T)0.0f;
+  }
+  return v;
+}
+
+template <class T, bool kTail>
+__device__ __forceinline__ void store_vec(T *p, typename Vec<T>::V v, int left) {
+  constexpr int N = Vec<T>::kN;
+  if (left >= N) {
+    *(typename Vec<T>::U *)p = v;
+  } else if (kTail) {
+#pragma unroll
+    for (int i = 0; i < N; i++)
+      if (i < left) p[i] = v[i];
+  }
+}
+
+template <int Ctrl>
+__device__ __forceinline__ float dppf(float v) {
+  return __builtin_bit_cast(
+      float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), Ctrl, 0xf, 0xf, true));
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
+constexpr int kRor8 = 0x128, kRor4 = 0x124, kRor2 = 0x122, kRor1 = 0x121;
+
+// Sums and maxima over groups of L lanes (16: one DPP row, 64: the
+// wavefront), the same in every lane of the group. Sums go down a fixed tree.
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
+  v += dppf<kRor8>(v);
+  v += dppf<kRor4>(v);
+  v += dppf<kRor2>(v);
+  v += dppf<kRor1>(v);
+  if (L == 64) {
+    v += __shfl_xor(v, 16);
+    v += __shfl_xor(v, 32);
+  }
+  return v;
+}
+template <int L>
+__device__ __forceinline__ float lanes_max(float v) {
+  v = fmaxf(v, dppf<kRor8>(v));
+  v = fmaxf(v, dppf<kRor4>(v));
+  v = fmaxf(v, dppf<kRor2>(v));
+  v = fmaxf(v, dppf<kRor1>(v));
+  if (L == 64) {
+    v = fmaxf(v, __shfl_xor(v, 16));
+    v = fmaxf(v, __shfl_xor(v, 32));
+  }
+  return v;
+}
+template <int L>
+__device__ __forceinline__ uint32_t lanes_min(uint32_t v) {
+  v = min(v, dpp<kRor8>(v));
+  v = min(v, dpp<kRor4>(v));
+  v = min(v, dpp<kRor2>(v));
+  v = min(v, dpp<kRor1>(v));
+  if (L == 64) {
+    v = min(v, (uint32_t)__shfl_xor((int)v, 16));
+    v = min(v, (uint32_t)__shfl_xor((int)v, 32));
+  }
+  return v;
+}
+
+}  // namespace taccl

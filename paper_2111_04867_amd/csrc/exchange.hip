@@ -1,0 +1,305 @@
+// Token rows into the expert buffer that an Alltoall sends (dispatch) and
+// back (combine), with combine's gradient.
+//
+//   dispatch: out[e_j, s_j] = x[t];  combine: out[t] = sum_j w_j buf[e_j, s_j]
+//   gradient: dbuf[e_j, s_j] = w_j dout[t],  dw_j = <dout[t], buf[e_j, s_j]>
+//
+// All three are bound by memory: a token's row is read (or written) once and
+// each of its k buffer rows written (or read) once, in 16-byte units. A row
+// whose length is no multiple of a unit has its last unit moved back to the
+// row's end, so that it overlaps the one before and holds the same values.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "elem.h"
+#include "expert.h"
+
+namespace taccl {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+typedef uint32_t Bits16 __attribute__((ext_vector_type(4)));
+typedef Bits16 Bits16u __attribute__((aligned(1)));
+
+// Units of a row: `unit` bytes each (16, or an element in a shorter row)
+struct RowUnits {
+  int64_t bytes;
+  int32_t unit, n;
+};
+RowUnits row_units(int64_t bytes, int element) {
+  const int unit = bytes >= 16 ? 16 : element;
+  return {bytes, unit, (int32_t)((bytes + unit - 1) / unit)};
+}
+
+__device__ __forceinline__ int64_t unit_at(const RowUnits &r, int u) {
+  const int64_t at = (int64_t)u * r.unit;
+  return at + r.unit > r.bytes ? r.bytes - r.unit : at;
+}
+
+// Row of choice (t, j) in the buffer, -1 without one
+__device__ __forceinline__ int64_t choice_row(int e, int s, int E, int64_t C) {
+  return (uint32_t)e < (uint32_t)E && s >= 0 && s < C ? (int64_t)e * C + s : -1;
+}
+
+__device__ __forceinline__ void store_unit(uint8_t *p, Bits16 v, int unit) {
+  if (unit == 16) *(Bits16u *)p = v;
+  else if (unit == 4) *(uint32_t *)p = v[0];
+  else if (unit == 2) *(uint16_t *)p = (uint16_t)v[0];
+  else *p = (uint8_t)v[0];
+}
+__device__ __forceinline__ Bits16 load_unit(const uint8_t *p, int unit) {
+  Bits16 v = {0, 0, 0, 0};
+  if (unit == 16) v = *(const Bits16u *)p;
+  else if (unit == 4) v[0] = *(const uint32_t *)p;
+  else if (unit == 2) v[0] = *(const uint16_t *)p;
+  else v[0] = *p;
+  return v;
+}
+
+// Rows of expert e from its count on, zeroed: `parts` blocks per expert, the
+// block at `b` takes every parts-th row.
+__device__ __forceinline__ void zero_rows(uint8_t *out, const RowUnits &r, const int32_t *counts,
+                                          int64_t C, int b, int parts) {
+  const int e = b / parts;
+  int64_t s = (int64_t)max(counts[e], 0) + b % parts;  // any 32-bit count
+  const Bits16 zero = {0, 0, 0, 0};
+  for (; s < C; s += parts)
+    for (int u = threadIdx.x; u < r.n; u += blockDim.x)
+      store_unit(out + (e * C + s) * r.bytes + unit_at(r, u), zero, r.unit);
+}
+
+struct DispatchArgs {
+  taccl_dispatch_t a;
+  RowUnits row, scale;
+  int lanes;        // threads per token row, a power of two up to kThreads
+  int token_blocks;  // blocks that take tokens; the rest zero rows
+  int parts;
+};
+
+template <int kK>
+__global__ __launch_bounds__(kThreads) void dispatch_kernel(DispatchArgs g) {
+  const taccl_dispatch_t &a = g.a;
+  if ((int)blockIdx.x >= g.token_blocks) {
+    const int b = blockIdx.x - g.token_blocks;
+    zero_rows((uint8_t *)a.out, g.row, a.counts, a.capacity, b, g.parts);
+    if (g.scale.n) zero_rows((uint8_t *)a.out_scale, g.scale, a.counts, a.capacity, b, g.parts);
+    return;
+  }
+  const int per = kThreads / g.lanes, lane = threadIdx.x & (g.lanes - 1);
+  const int64_t t = (int64_t)blockIdx.x * per + threadIdx.x / g.lanes;
+  if (t >= a.tokens) return;
+  int64_t to[kK];
+#pragma unroll
+  for (int j = 0; j < kK; j++)
+    to[j] = j < a.k ? choice_row(a.experts[t * a.k + j], a.slots[t * a.k + j], a.num_experts,
+                                 a.capacity)
+                    : -1;
+  const uint8_t *x = (const uint8_t *)a.x + t * a.x_stride * a.element_bytes;
+  for (int u = lane; u < g.row.n + g.scale.n; u += g.lanes) {
+    const bool scale = u >= g.row.n;
+    const RowUnits &r = scale ? g.scale : g.row;
+    const int64_t at = unit_at(r, scale ? u - g.row.n : u);
+    const uint8_t *from = scale ? (const uint8_t *)(a.scale + t * a.scale_stride) : x;
+    uint8_t *out = scale ? (uint8_t *)a.out_scale : (uint8_t *)a.out;
+    const Bits16 v = load_unit(from + at, r.unit);
+#pragma unroll
+    for (int j = 0; j < kK; j++)
+      if (to[j] >= 0) store_unit(out + to[j] * r.bytes + at, v, r.unit);
+  }
+}
+
+struct CombineArgs {
+  taccl_combine_t a;
+  int lanes;  // threads per token row
+};
+
+template <class T, int kK, bool kTail>
+__global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs g) {
+  constexpr int N = Vec<T>::kN;
+  const taccl_combine_t &a = g.a;
+  const int per = kThreads / g.lanes, lane = threadIdx.x & (g.lanes - 1), D = a.cols;
+  const int64_t t = (int64_t)blockIdx.x * per + threadIdx.x / g.lanes;
+  if (t >= a.tokens) return;
+  int64_t from[kK];
+  float w[kK];
+#pragma unroll
+  for (int j = 0; j < kK; j++) {
+    from[j] = j < a.k ? choice_row(a.experts[t * a.k + j], a.slots[t * a.k + j], a.num_experts,
+                                   a.capacity)
+                      : -1;
+    w[j] = j < a.k && a.weights ? a.weights[t * a.k + j] : 1.0f;
+  }
+  for (int u = lane; u * N < D; u += g.lanes) {
+    const int c = u * N;
+    float s[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) s[i] = 0;
+    typename Vec<T>::V v[kK];
+#pragma unroll
+    for (int j = 0; j < kK; j++)
+      if (from[j] >= 0) v[j] = load_vec<T, kTail>((const T *)a.buffer + from[j] * D + c, D - c);
+#pragma unroll
+    for (int j = 0; j < kK; j++)
+      if (from[j] >= 0) {
+#pragma unroll
+        for (int i = 0; i < N; i++) s[i] += w[j] * (float)v[j][i];
+      }
+    typename Vec<T>::V o;
+#pragma unroll
+    for (int i = 0; i < N; i++) o[i] = (T)s[i];
+    store_vec<T, kTail>((T *)a.out + t * a.out_stride + c, o, D - c);
+  }
+}
+
+struct CombineBackwardArgs {
+  taccl_combine_backward_t a;
+  RowUnits row;
+  int token_blocks, parts;
+};
+
+// kWaves wavefronts per token
+template <class T, int kK, int kWaves, bool kTail>
+__global__ __launch_bounds__(kThreads) void combine_backward_kernel(CombineBackwardArgs g) {
+  constexpr int N = Vec<T>::kN, kTokens = kThreads / 64 / kWaves;
+  __shared__ float red[kThreads / 64][kK];
+  const taccl_combine_backward_t &a = g.a;
+  if ((int)blockIdx.x >= g.token_blocks) {
+    zero_rows((uint8_t *)a.dbuffer, g.row, a.counts, a.capacity, blockIdx.x - g.token_blocks,
+              g.parts);
+    return;
+  }
+  const int lane = threadIdx.x % (64 * kWaves), D = a.cols;
+  const int64_t t = (int64_t)blockIdx.x * kTokens + threadIdx.x / (64 * kWaves);
+  if (kWaves == 1 && t >= a.tokens) return;  // else a block is one token
+  int64_t at[kK];
+  float w[kK], dot[kK];
+#pragma unroll
+  for (int j = 0; j < kK; j++) {
+    at[j] = j < a.k ? choice_row(a.experts[t * a.k + j], a.slots[t * a.k + j], a.num_experts,
+                                 a.capacity)
+                    : -1;
+    w[j] = j < a.k ? a.weights[t * a.k + j] : 0.0f;
+    dot[j] = 0;
+  }
+  for (int u = lane; u * N < D; u += 64 * kWaves) {
+    const int c = u * N;
+    const auto d = load_vec<T, kTail>((const T *)a.dout + t * a.dout_stride + c, D - c);
+    typename Vec<T>::V v[kK];
+#pragma unroll
+    for (int j = 0; j < kK; j++)
+      if (at[j] >= 0) v[j] = load_vec<T, kTail>((const T *)a.buffer + at[j] * D + c, D - c);
+#pragma unroll
+    for (int j = 0; j < kK; j++)
+      if (at[j] >= 0) {
+        typename Vec<T>::V o;
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+          o[i] = (T)(w[j] * (float)d[i]);
+          dot[j] += (float)d[i] * (float)v[j][i];
+        }
+        store_vec<T, kTail>((T *)a.dbuffer + at[j] * D + c, o, D - c);
+      }
+  }
+#pragma unroll
+  for (int j = 0; j < kK; j++) dot[j] = lanes_sum<64>(dot[j]);
+  if (kWaves > 1) {
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int j = 0; j < kK; j++) red[threadIdx.x >> 6][j] = dot[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kK; j++)
+      for (int i = 1; i < kWaves; i++) dot[j] = i == 1 ? red[0][j] + red[1][j] : dot[j] + red[i][j];
+  }
+#pragma unroll
+  for (int j = 0; j < kK; j++)
+    if (lane == j && j < a.k) a.dweights[t * a.k + j] = dot[j];
+}
+
+// Threads per token row: enough for one unit each, at most a block
+int row_lanes(int64_t units) {
+  int lanes = 1;
+  while (lanes < kThreads && lanes < units) lanes *= 2;
+  return lanes;
+}
+
+// Blocks per expert that zero rows: about four per CU in all
+int zero_parts(int64_t capacity, int E, int cus) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(capacity, (4 * (int64_t)cus + E - 1) / E));
+}
+
+#define BY_CHOICES(k, F) \
+  ((k) <= 1 ? F(1) : (k) <= 2 ? F(2) : (k) <= 4 ? F(4) : (k) <= 8 ? F(8) : F(16))
+
+template <class T>
+const void *combine_fn(int k, int cols) {
+  const bool tail = cols % Vec<T>::kN != 0;
+#define F(K) (tail ? (const void *)combine_kernel<T, K, true> : (const void *)combine_kernel<T, K, false>)
+  return BY_CHOICES(k, F);
+#undef F
+}
+template <class T>
+const void *combine_backward_fn(int k, int cols, bool wide) {
+  const bool tail = cols % Vec<T>::kN != 0;
+#define G(K, W)                                                     \
+  (tail ? (const void *)combine_backward_kernel<T, K, W, true>      \
+        : (const void *)combine_backward_kernel<T, K, W, false>)
+#define F(K) (wide ? G(K, 4) : G(K, 1))
+  return BY_CHOICES(k, F);
+#undef F
+#undef G
+}
+
+}  // namespace
+
+hipError_t launch_dispatch(const taccl_dispatch_t &a, int cus, hipStream_t stream) {
+  DispatchArgs g{a, row_units((int64_t)a.cols * a.element_bytes, a.element_bytes), {0, 4, 0}, 1, 0, 1};
+  if (a.scale_cols) g.scale = row_units(4 * (int64_t)a.scale_cols, 4);
+  g.lanes = row_lanes(g.row.n + g.scale.n);
+  const int64_t per = kThreads / g.lanes;
+  g.token_blocks = (int)((a.tokens + per - 1) / per);
+  g.parts = zero_parts(a.capacity, a.num_experts, cus);
+#define F(K) (const void *)dispatch_kernel<K>
+  const void *fn = BY_CHOICES(a.k, F);
+#undef F
+  void *args[] = {&g};
+  return hipLaunchKernel(fn, dim3((uint32_t)g.token_blocks + (uint32_t)a.num_experts * g.parts),
+                         dim3(kThreads), args, 0, stream);
+}
+
+hipError_t launch_combine(const taccl_combine_t &a, hipStream_t stream) {
+  CombineArgs g{a, 1};
+  const int n = a.dtype == TACCL_F32 ? 4 : 8;
+  g.lanes = row_lanes((a.cols + n - 1) / n);
+  const int64_t per = kThreads / g.lanes;
+  const void *fn = a.dtype == TACCL_F32    ? combine_fn<float>(a.k, a.cols)
+                   : a.dtype == TACCL_BF16 ? combine_fn<bf16_t>(a.k, a.cols)
+                                           : combine_fn<f16_t>(a.k, a.cols);
+  void *args[] = {&g};
+  return hipLaunchKernel(fn, dim3((uint32_t)((a.tokens + per - 1) / per)), dim3(kThreads), args, 0,
+                         stream);
+}
+
+hipError_t launch_combine_backward(const taccl_combine_backward_t &a, int cus,
+                                   hipStream_t stream) {
+  CombineBackwardArgs g{a, {}, 0, 1};
+  const int size = a.dtype == TACCL_F32 ? 4 : 2;
+  g.row = row_units((int64_t)a.cols * size, size);
+  // a block per token where tokens are few and rows long
+  const bool wide = a.tokens < 4 * (int64_t)cus && g.row.n > 64;
+  const int64_t per = wide ? 1 : kThreads / 64;
+  g.token_blocks = (int)((a.tokens + per - 1) / per);
+  g.parts = zero_parts(a.capacity, a.num_experts, cus);
+  const void *fn = a.dtype == TACCL_F32    ? combine_backward_fn<float>(a.k, a.cols, wide)
+                   : a.dtype == TACCL_BF16 ? combine_backward_fn<bf16_t>(a.k, a.cols, wide)
+                                           : combine_backward_fn<f16_t>(a.k, a.cols, wide);
+  void *args[] = {&g};
+  return hipLaunchKernel(fn, dim3((uint32_t)g.token_blocks + (uint32_t)a.num_experts * g.parts),
+                         dim3(kThreads), args, 0, stream);
+}
+
+}  // namespace taccl
