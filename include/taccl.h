@@ -395,7 +395,7 @@ taccl_status_t taccl_norm(const taccl_norm_t *a, taccl_stream_t stream);
  *   dx = dtotal + r * a - h * r^3 * mean(a * h),  dweight = sum over rows of
  *   dout * h * r (32-bit floats; zero without rows).
  * dx may be dout, dtotal or h itself, with the same stride. `workspace`:
- * taccl_norm_workspace(cols) bytes, 4-byte aligned, not shared with another
+ * taccl_norm_workspace(cols) bytes, 16-byte aligned, not shared with another
  * call in flight.
  */
 typedef struct {
@@ -433,7 +433,7 @@ int64_t taccl_norm_workspace(int32_t cols);
  * Tokens with mask 0, and tokens whose logits are all minus infinity, choose
  * nothing and count nowhere; nothing of a masked token's logits is used.
  * 1 <= E <= 1024, 1 <= k <= min(E, 16), tokens <= 2^21.
- * `workspace`: taccl_route_workspace(E) bytes, 4-byte aligned, not shared
+ * `workspace`: taccl_route_workspace(E) bytes, 16-byte aligned, not shared
  * with another call in flight.
  */
 typedef struct {

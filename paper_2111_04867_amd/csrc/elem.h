@@ -24,15 +24,42 @@ struct Vec {
 
 // The vector at p. Of the columns from `left` on nothing is read or written
 // and they come as zero; kTail: fewer than kN may be left (else none or kN).
+// Such a rest is read and written as its binary digits: 4, 2 and 1 elements.
 template <class T, bool kTail>
 __device__ __forceinline__ typename Vec<T>::V load_vec(const T *p, int left) {
   constexpr int N = Vec<T>::kN;
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  typedef T T2 __attribute__((ext_vector_type(2)));
+  typedef T4 U4 __attribute__((aligned(sizeof(T))));
+  typedef T2 U2 __attribute__((aligned(sizeof(T))));
   typename Vec<T>::V v;
+#pragma unroll
+  for (int i = 0; i < N; i++) v[i] = (T)0.0f;
   if (left >= N) {
     v = *(const typename Vec<T>::U *)p;
-  } else {
+  } else if (kTail && left > 0) {
+    T4 w4 = {(T)0.0f, (T)0.0f, (T)0.0f, (T)0.0f};
+    T2 w2 = {(T)0.0f, (T)0.0f};
+    T w1 = (T)0.0f;
+    if (N == 8 && (left & 4)) w4 = *(const U4 *)p;
+    if (left & 2) w2 = *(const U2 *)(p + (left & 4));
+    if (left & 1) w1 = p[left & 6];
+    if constexpr (N == 8) {
 #pragma unroll
-    for (int i = 0; i < N; i++) v[i] = kTail && i < left ? p[i] : (T)0.0f;
+      for (int i = 0; i < 4; i++) v[i] = w4[i];
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        v[i] = left & 4 ? v[i] : w2[i];
+        v[4 + i] = left & 4 ? w2[i] : (T)0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) v[i] = (left & 1) && (left & 6) == i ? w1 : v[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; i++) v[i] = w2[i];
+      v[0] = left == 1 ? w1 : v[0];
+      v[2] = left == 3 ? w1 : (T)0.0f;
+    }
   }
   return v;
 }
@@ -40,13 +67,35 @@ __device__ __forceinline__ typename Vec<T>::V load_vec(const T *p, int left) {
 template <class T, bool kTail>
 __device__ __forceinline__ void store_vec(T *p, typename Vec<T>::V v, int left) {
   constexpr int N = Vec<T>::kN;
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  typedef T T2 __attribute__((ext_vector_type(2)));
+  typedef T4 U4 __attribute__((aligned(sizeof(T))));
+  typedef T2 U2 __attribute__((aligned(sizeof(T))));
   if (left >= N) {
     *(typename Vec<T>::U *)p = v;
-  } else if (kTail) {
+  } else if (kTail && left > 0) {
+    T2 w2 = {v[0], v[1]};
+    T w1 = v[0];
+    if constexpr (N == 8) {
+      if (left & 4) {
+        *(U4 *)p = T4{v[0], v[1], v[2], v[3]};
+        w2 = T2{v[4], v[5]};
+      }
 #pragma unroll
-    for (int i = 0; i < N; i++)
-      if (i < left) p[i] = v[i];
+      for (int i = 2; i < 8; i += 2) w1 = (left & 6) == i ? v[i] : w1;
+    } else {
+      w1 = left & 2 ? v[2] : w1;
+    }
+    if (left & 2) *(U2 *)(p + (left & 4)) = w2;
+    if (left & 1) p[left & 6] = w1;
   }
+}
+
+// The same vector, whose conversions to float are not kept across this point:
+// 16-bit rows held as they are stored take half the registers.
+template <class V>
+__device__ __forceinline__ void as_stored(V &v) {
+  asm volatile("" : "+v"(v));
 }
 
 template <int Ctrl>

@@ -44,7 +44,7 @@ struct Check {
     limit(k > kMaxChoices, "more than 16 choices per token");
   }
   void workspace(const void *p, int64_t bytes, int64_t need) {
-    array(p, 4, "workspace");
+    array(p, 16, "workspace");
     invalid(bytes < need, "workspace too small");
   }
 };
@@ -155,7 +155,8 @@ taccl_status_t taccl_norm_backward(const taccl_norm_backward_t *a, taccl_stream_
 }
 
 int64_t taccl_route_workspace(int32_t num_experts) {
-  return num_experts < 1 ? 0 : 4 * (int64_t)kRouteMaxBlocks * (2 * (int64_t)num_experts + 1);
+  const int64_t wide = ((int64_t)num_experts + 7) / 8 * 8;  // 6 bytes each, and a count
+  return num_experts < 1 ? 0 : kRouteMaxBlocks * (8 * wide + 4);
 }
 
 taccl_status_t taccl_route(const taccl_route_t *a, taccl_stream_t stream) {

@@ -6,7 +6,17 @@
 //
 // A row is held in registers between its two passes (statistics, outputs), so
 // memory is read and written once: kTpr threads per row, kNv vectors of 16
-// bytes each.
+// bytes each. Both kernels are bound by memory.
+//
+// Forward: one vector per thread as far as a block reaches. 8192 x 4096 bf16
+// with residual and 8-bit copy (303 MB): 512 threads 59.9 us (5.05 TB/s, the
+// rate of a large copy), 256 threads with two vectors 63.5 us, 128 with four
+// 68.4 us, a wavefront with eight 80.6 us: what counts is wavefronts in flight.
+// Gradient: four vectors per thread, so that a block of two to four rows needs
+// few partial sums of dw, and 16-bit rows stay as they are stored (as_stored).
+// 8192 x 2048 bf16: 31.1 us for both launches (134 MB; 27 us the first), a
+// block per row 36 us; 8192 x 4096: 55.1 us with 128 threads per row, 58 us
+// with 256, 71 us with a wavefront.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -39,6 +49,7 @@ __device__ __forceinline__ void row_reduce(float &v, float &m, float *red) {
     red[2 * w + 1] = m;
   }
   __syncthreads();
+  red += 2 * (threadIdx.x / kTpr * (kTpr / 64));
   v = red[0];
   m = red[1];
 #pragma unroll
@@ -85,7 +96,7 @@ __device__ __forceinline__ void store_f8(uint8_t *p, const float *y, float inv, 
 template <class T, int kTpr, int kNv, bool kTail>
 __global__ __launch_bounds__(block_threads(kTpr)) void norm_kernel(taccl_norm_t a) {
   constexpr int N = Vec<T>::kN, kRows = block_threads(kTpr) / kTpr;
-  __shared__ float red[2 * (kTpr / 64 + 1)];
+  __shared__ float red[2 * (block_threads(kTpr) / 64)];
   const int lane = threadIdx.x % kTpr, D = a.cols;
   const int64_t at = (int64_t)blockIdx.x * kRows + threadIdx.x / kTpr;
   const bool live = at < a.rows;
@@ -152,20 +163,29 @@ __global__ __launch_bounds__(block_threads(kTpr)) void norm_kernel(taccl_norm_t 
 }
 
 // Gradient: blocks take rows in turn; each thread sums its columns of dw
-// over its rows, and a block's sums go to one row of `partial`.
+// over its rows, and a block's sums go to one row of `partial`. Columns past
+// the last whole vector (kTail) go to the row's first lanes, one each: their
+// vector in pieces, behind branches among the loads, took 4 us more for 3001
+// rows of 1999 columns.
 template <class T, int kTpr, int kNv, bool kTail>
 __global__ __launch_bounds__(block_threads(kTpr)) void norm_backward_kernel(
     taccl_norm_backward_t a, float *partial) {
   constexpr int N = Vec<T>::kN, kRows = block_threads(kTpr) / kTpr;
-  __shared__ float red[2][2 * (kTpr / 64 + 1)];
-  __shared__ float sums[kRows > 1 ? kTpr * kNv * N : 1];
-  const int lane = threadIdx.x % kTpr, sub = threadIdx.x / kTpr, D = a.cols;
+  __shared__ float red[2][2 * (block_threads(kTpr) / 64)];
+  constexpr int kCols = kTpr * kNv * N;
+  __shared__ __align__(16) float sums[kRows > 1 ? kRows * kCols : 1];
+  __shared__ float tail[kRows][N];
+  const int lane = threadIdx.x % kTpr, sub = threadIdx.x / kTpr;
+  const int D = a.cols, whole = kTail ? D / N * N : D;
+  const bool more = kTail && lane < D - whole;  // has column whole + lane
+  const T *w = (const T *)a.weight;
   typename Vec<T>::V wv[kNv];
-  float acc[kNv][N];
+  float acc[kNv][N], acc1 = 0;
+  const float w1 = more ? (float)w[whole + lane] : 0.0f;
 #pragma unroll
   for (int j = 0; j < kNv; j++) {
     const int c = N * (lane + kTpr * j);
-    wv[j] = load_vec<T, kTail>((const T *)a.weight + c, D - c);
+    wv[j] = load_vec<T, false>(w + c, whole - c);
 #pragma unroll
     for (int i = 0; i < N; i++) acc[j][i] = 0;
   }
@@ -176,13 +196,27 @@ __global__ __launch_bounds__(block_threads(kTpr)) void norm_backward_kernel(
     const int64_t row = live ? first + sub : a.rows - 1;
     const T *dy = (const T *)a.dout + row * a.dout_stride;
     const T *h = (const T *)a.h + row * a.h_stride;
-    typename Vec<T>::V dv[kNv], hv[kNv];
-    float ss = 0, dot = 0;
+    const T *dt = a.dtotal ? (const T *)a.dtotal + row * a.dtotal_stride : nullptr;
+    T *dx = (T *)a.dx + row * a.dx_stride;
+    typename Vec<T>::V dv[kNv], hv[kNv], tv[kNv];
+    float ss = 0, dot = 0, d1 = 0, h1 = 0, t1 = 0;
 #pragma unroll
     for (int j = 0; j < kNv; j++) {
       const int c = N * (lane + kTpr * j);
-      dv[j] = load_vec<T, kTail>(dy + c, D - c);
-      hv[j] = load_vec<T, kTail>(h + c, D - c);
+      dv[j] = load_vec<T, false>(dy + c, whole - c);
+      hv[j] = load_vec<T, false>(h + c, whole - c);
+    }
+    if (dt) {
+#pragma unroll
+      for (int j = 0; j < kNv; j++) {
+        const int c = N * (lane + kTpr * j);
+        tv[j] = load_vec<T, false>(dt + c, whole - c);
+      }
+    }
+    if (more) {
+      d1 = (float)dy[whole + lane];
+      h1 = (float)h[whole + lane];
+      if (dt) t1 = (float)dt[whole + lane];
     }
 #pragma unroll
     for (int j = 0; j < kNv; j++)
@@ -192,65 +226,99 @@ __global__ __launch_bounds__(block_threads(kTpr)) void norm_backward_kernel(
         ss += x * x;
         dot += x * ((float)dv[j][i] * (float)wv[j][i]);
       }
+    if (kTail) {
+      ss += h1 * h1;
+      dot += h1 * (d1 * w1);
+    }
+#pragma unroll
+    for (int j = 0; j < kNv; j++) {
+      as_stored(dv[j]);
+      as_stored(hv[j]);
+      as_stored(wv[j]);
+    }
     row_reduce<kTpr, false>(ss, dot, red[turn]);
     const float r = 1.0f / sqrtf(ss / (float)D + a.eps);
     const float f = r * r * r * (dot / (float)D);
 #pragma unroll
     for (int j = 0; j < kNv; j++) {
-      const int c = N * (lane + kTpr * j), left = live ? D - c : 0;
-      typename Vec<T>::V o, t;
-      if (a.dtotal) t = load_vec<T, kTail>((const T *)a.dtotal + row * a.dtotal_stride + c, left);
+      const int c = N * (lane + kTpr * j);
+      typename Vec<T>::V o;
 #pragma unroll
       for (int i = 0; i < N; i++) {
         const float x = (float)hv[j][i], d = (float)dv[j][i];
         float g = r * (d * (float)wv[j][i]) - x * f;
-        if (a.dtotal) g += (float)t[i];
+        if (dt) g += (float)tv[j][i];
         o[i] = (T)g;
         if (live) acc[j][i] += d * (x * r);
       }
-      store_vec<T, kTail>((T *)a.dx + row * a.dx_stride + c, o, left);
+      store_vec<T, false>(dx + c, o, live ? whole - c : 0);
+    }
+    if (more && live) {
+      dx[whole + lane] = (T)(r * (d1 * w1) - h1 * f + t1);
+      acc1 += d1 * (h1 * r);
     }
   }
   float *out = partial + (int64_t)blockIdx.x * D;
   if (kRows == 1) {
 #pragma unroll
-    for (int j = 0; j < kNv; j++)
+    for (int j = 0; j < kNv; j++) {
+      const int c = N * (lane + kTpr * j);
+      if (c < whole) {
 #pragma unroll
-      for (int i = 0; i < N; i++) {
-        const int c = N * (lane + kTpr * j) + i;
-        if (c < D) out[c] = acc[j][i];
+        for (int i = 0; i < N; i++) out[c + i] = acc[j][i];
       }
+    }
+    if (more) out[whole + lane] = acc1;
     return;
   }
-  for (int s = 0; s < kRows; s++) {  // the rows' sums in order
-    if (sub == s) {
+  // the sums of the block's rows, in order
+  float *own = sums + sub * kCols;
 #pragma unroll
-      for (int j = 0; j < kNv; j++)
+  for (int j = 0; j < kNv; j++)
 #pragma unroll
-        for (int i = 0; i < N; i++) {
-          const int c = N * (lane + kTpr * j) + i;
-          sums[c] = s ? sums[c] + acc[j][i] : acc[j][i];
-        }
-    }
-    __syncthreads();
+    for (int i = 0; i < N; i++) own[N * (lane + kTpr * j) + i] = acc[j][i];
+  if (more) tail[sub][lane] = acc1;
+  __syncthreads();
+  for (int c = threadIdx.x; c < D; c += blockDim.x) {
+    float s = 0;
+#pragma unroll
+    for (int i = 0; i < kRows; i++) s += c < whole ? sums[i * kCols + c] : tail[i][c - whole];
+    out[c] = s;
   }
-  for (int c = threadIdx.x; c < D; c += blockDim.x) out[c] = sums[c];
 }
 
 // Columns of `partial` [n][cols] summed in a fixed order: 64 columns per
-// block, 16 rows at a time.
+// block, 64 rows at a time, four of them on their way per thread.
 __global__ __launch_bounds__(1024) void column_sums_kernel(const float *partial, int n, int cols,
                                                            float *out) {
-  __shared__ float part[16][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), slice = threadIdx.x >> 6;
-  float s = 0;
-  if (c < cols)
-    for (int i = slice; i < n; i += 16) s += partial[(int64_t)i * cols + c];
-  part[slice][threadIdx.x & 63] = s;
+  __shared__ float part[64][64];
+  const int c = blockIdx.x * 64 + 4 * (threadIdx.x & 15), slice = threadIdx.x >> 4;
+  float s[4] = {0, 0, 0, 0};
+  for (int i = slice; i < n; i += 256) {
+    Vec<float>::V v[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++)
+      v[j] = load_vec<float, true>(partial + (int64_t)min(i + 64 * j, n - 1) * cols + c, cols - c);
+#pragma unroll
+    for (int j = 0; j < 4; j++)
+      if (i + 64 * j < n) {
+#pragma unroll
+        for (int x = 0; x < 4; x++) s[x] += v[j][x];
+      }
+  }
+#pragma unroll
+  for (int x = 0; x < 4; x++) part[slice][4 * (threadIdx.x & 15) + x] = s[x];
   __syncthreads();
-  if (slice == 0 && c < cols) {
-    for (int i = 1; i < 16; i++) s += part[i][threadIdx.x];
-    out[c] = s;
+  const int col = threadIdx.x & 63, w = threadIdx.x >> 6;
+  float t = 0;
+#pragma unroll
+  for (int i = 0; i < 4; i++) t += part[4 * w + i][col];
+  __syncthreads();
+  part[w][col] = t;
+  __syncthreads();
+  if (w == 0 && blockIdx.x * 64 + col < cols) {
+    for (int i = 1; i < 16; i++) t += part[i][col];
+    out[blockIdx.x * 64 + col] = t;
   }
 }
 
@@ -259,27 +327,42 @@ struct RowShape {
   int tpr, nv;
 };
 template <class T>
-RowShape row_shape(int cols) {
+RowShape row_shape(int cols, bool backward) {
   const int v = (cols + Vec<T>::kN - 1) / Vec<T>::kN;
   if (v <= 16) return {16, 1};
   if (v <= 64) return {64, 1};
-  if (v <= 128) return {64, 2};
+  if (backward) {
+    if (v <= 128) return {64, 2};
+    if (v <= 256) return {64, 4};
+    if (v <= 512) return {128, 4};
+    if (v <= 1024) return {256, 4};
+    if (v <= 2048) return {512, 4};
+    return {512, 8};  // 32-bit rows only
+  }
+  if (v <= 128) return {128, 1};
   if (v <= 256) return {256, 1};
-  if (v <= 512) return {256, 2};
-  if (v <= 1024) return {256, 4};
-  if (v <= 2048) return {512, 4};
-  return {512, 8};  // 32-bit rows only
+  if (v <= 512) return {512, 1};
+  if (v <= 1024) return {1024, 1};
+  if (v <= 2048) return {1024, 2};
+  return {1024, 4};  // 32-bit rows only
 }
 
-#define NORM_SHAPES(F) F(16, 1) F(64, 1) F(64, 2) F(256, 1) F(256, 2) F(256, 4) F(512, 4)
-
 template <class T, bool kTail>
-const void *norm_fn(RowShape s, bool backward) {
-#define PICK(TPR, NV)                                                    \
-  if (s.tpr == TPR && s.nv == NV)                                        \
-    return backward ? (const void *)norm_backward_kernel<T, TPR, NV, kTail> \
-                    : (const void *)norm_kernel<T, TPR, NV, kTail>;
-  NORM_SHAPES(PICK)
+const void *norm_fn(RowShape s) {
+#define PICK(TPR, NV) \
+  if (s.tpr == TPR && s.nv == NV) return (const void *)norm_kernel<T, TPR, NV, kTail>;
+  PICK(16, 1) PICK(64, 1) PICK(128, 1) PICK(256, 1) PICK(512, 1) PICK(1024, 1) PICK(1024, 2)
+  if constexpr (sizeof(T) == 4) {
+    PICK(1024, 4)
+  }
+#undef PICK
+  return nullptr;
+}
+template <class T, bool kTail>
+const void *norm_backward_fn(RowShape s) {
+#define PICK(TPR, NV) \
+  if (s.tpr == TPR && s.nv == NV) return (const void *)norm_backward_kernel<T, TPR, NV, kTail>;
+  PICK(16, 1) PICK(64, 1) PICK(64, 2) PICK(64, 4) PICK(128, 4) PICK(256, 4) PICK(512, 4)
   if constexpr (sizeof(T) == 4) {
     PICK(512, 8)
   }
@@ -289,8 +372,9 @@ const void *norm_fn(RowShape s, bool backward) {
 
 template <class T>
 const void *norm_pick_type(int cols, bool backward, RowShape &s) {
-  s = row_shape<T>(cols);
-  return cols % Vec<T>::kN ? norm_fn<T, true>(s, backward) : norm_fn<T, false>(s, backward);
+  s = row_shape<T>(cols, backward);
+  if (cols % Vec<T>::kN) return backward ? norm_backward_fn<T, true>(s) : norm_fn<T, true>(s);
+  return backward ? norm_backward_fn<T, false>(s) : norm_fn<T, false>(s);
 }
 
 const void *norm_pick(int dtype, int cols, bool backward, RowShape &s) {

@@ -23,13 +23,16 @@ namespace {
 
 constexpr int kRouteThreads = 1024;
 constexpr int kBackThreads = 256;
+constexpr int kSmallTile = 16, kOneBlock = 128, kSmallBlocks = 8192;
 
-// per-block results: the experts' counts with the rows' count behind them,
-// and the experts' probability sums
+// Per-block results: the experts' counts and probability sums in rows padded
+// to whole 16-byte vectors, and the tokens that count.
 struct RoutePartial {
-  uint32_t *counts;  // [blocks][E + 1]
-  float *sums;       // [blocks][E]
-  int per_block;     // tokens per block
+  float *sums;       // [blocks][wide]
+  uint32_t *rows;    // [blocks]
+  uint16_t *counts;  // [blocks][wide]
+  int wide;
+  int per_block;  // tokens per block
   int blocks;
 };
 
@@ -82,9 +85,97 @@ struct TokenRow {
   }
 };
 
+// Rank (0 = largest) of `key` in its row of 16 lanes, equal keys by lane
+__device__ __forceinline__ int row_rank(int key, int lane) {
+  int rank = 0;
+#define BEATEN(R) \
+  rank += (int)dpp<0x120 + R>((uint32_t)key) > (lane >= R ? key - 1 : key) ? 1 : 0;
+  BEATEN(1) BEATEN(2) BEATEN(3) BEATEN(4) BEATEN(5) BEATEN(6) BEATEN(7) BEATEN(8)
+  BEATEN(9) BEATEN(10) BEATEN(11) BEATEN(12) BEATEN(13) BEATEN(14) BEATEN(15)
+#undef BEATEN
+  return rank;
+}
+// floats as integers in the same order (both zeros alike, no NaN); kNone is
+// below minus infinity's
+constexpr int kNone = -0x7FFFFFFF;
+__device__ __forceinline__ int order_key(float v) {
+  const int x = __builtin_bit_cast(int, v + 0.0f);
+  return x ^ ((x >> 31) & 0x7FFFFFFF);
+}
+
+// A lane's choice: rank among the token's choices, expert (-1: none) and logit
+struct Choice {
+  int rank, expert;
+  float logit;
+};
+
+// One at a time: the row's maximum k times. Changes v.
+template <int kL, int kEpl>
+__device__ __forceinline__ Choice choose_each(float *v, int k, int lane) {
+  Choice c{lane, -1, 0.0f};
+  for (int j = 0; j < k; j++) {
+    float m = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < kEpl; i++) m = fmaxf(m, v[i]);
+    m = lanes_max<kL>(m);
+    uint32_t at = 0xFFFFFFFFu;
+#pragma unroll
+    for (int i = kEpl - 1; i >= 0; i--) at = v[i] == m ? (uint32_t)(lane * kEpl + i) : at;
+    at = lanes_min<kL>(at);
+    if (m == -__builtin_inff()) at = 0xFFFFFFFFu;
+#pragma unroll
+    for (int i = 0; i < kEpl; i++)
+      v[i] = at == (uint32_t)(lane * kEpl + i) ? -__builtin_inff() : v[i];
+    if (lane == j && at != 0xFFFFFFFFu) {
+      c.expert = (int)at;
+      c.logit = m;
+    }
+  }
+  return c;
+}
+
+// By a threshold: the k-th largest of the 16 lanes' maxima bounds the k-th
+// largest logit from below, so the choices are among the logits that reach it.
+// Where at most 16 do (for k = 8 about 11 of 256 random ones), one lane takes
+// each, in the order of their index, and their ranks are the choice. False:
+// some row of the wavefront has more.
+template <class T, int kEpl>
+__device__ __forceinline__ bool choose_ranked(const float *v, int k, int lane, const T *row,
+                                              uint16_t *list, Choice &c) {
+  float m = -__builtin_inff();
+#pragma unroll
+  for (int i = 0; i < kEpl; i++) m = fmaxf(m, v[i]);
+  const int top = row_rank(order_key(m), lane);
+  // at least the lowest number: minus infinities are never chosen
+  const float bound = lanes_max<16>(top == k - 1 ? fmaxf(m, -__FLT_MAX__) : -__FLT_MAX__);
+  uint32_t hit = 0;
+#pragma unroll
+  for (int i = 0; i < kEpl; i++)
+    hit |= v[i] >= bound ? 1u << i : 0u;
+  const uint32_t mine = __popc(hit), upto = row_scan_add(mine);
+  const uint32_t all = dpp<0x15F>(upto);  // the row's last lane
+  if (__any(all > 16)) return false;
+  for (uint32_t at = upto - mine; __any(hit); hit &= hit - 1, at++)
+    if (hit) list[at] = (uint16_t)(lane * kEpl + __ffs(hit) - 1);
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("" ::: "memory");  // one wavefront's LDS accesses are in order
+  c = Choice{lane, -1, 0.0f};
+  int key = kNone;
+  if ((uint32_t)lane < all) {
+    c.expert = list[lane];
+    c.logit = (float)row[c.expert];
+    key = order_key(c.logit);
+  }
+  const int rank = row_rank(key, lane);
+  if ((uint32_t)lane < all) c.rank = rank;
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("" ::: "memory");
+  return true;
+}
+
 // The balance loss and the totals from the experts' counts and sums in LDS
 __device__ __forceinline__ void finish_loss(const taccl_route_t &a, const uint32_t *cnt,
-                                            const float *sums, float *red) {
+                                            const float *sums, uint32_t rows, float *red) {
   const int E = a.num_experts;
   float s = 0;
   for (int e = threadIdx.x; e < E; e += blockDim.x) {
@@ -97,28 +188,33 @@ __device__ __forceinline__ void finish_loss(const taccl_route_t &a, const uint32
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int i = 1; i < (int)blockDim.x / 64; i++) s += red[i];
-    const float n = (float)max(cnt[E], 1u);
+    const float n = (float)max(rows, 1u);
     *a.loss = a.coef * (float)E * (s / (n * (float)a.k) / n);
-    *a.rows = (int32_t)cnt[E];
+    *a.rows = (int32_t)rows;
   }
 }
 
-// First launch: per block of tokens. A tile is one token per group of lanes;
-// the tile's choices of an expert are bits of one word per expert in LDS, so
-// a choice's place is the count of the tiles before plus the bits below its
-// own. A single block writes the final results.
-template <class T, int kL, int kEpl>
+// First launch: per block of tokens. The block's wavefronts take tokens on
+// their own, up to kStep of the block, and leave every choice as a bit of the
+// expert's words in LDS (one bit per token). A choice's place in the block is
+// then the count of the steps before plus the bits below its own. A single
+// block writes the final results.
+constexpr int kStep = 256, kWords = kStep / 64;
+
+template <class T, int kL, int kEpl, bool kRanked>
 __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, RoutePartial part) {
-  constexpr int kGroups = kRouteThreads / kL, kWaves = kRouteThreads / 64;
-  constexpr int kCols = kL * kEpl;
-  __shared__ uint64_t bits[kCols + 1];
+  constexpr int kWaves = kRouteThreads / 64, kCols = kL * kEpl;
+  __shared__ uint64_t bits[kCols + 1][kWords];
   __shared__ uint32_t cnt[kCols + 1];
   __shared__ float sums[kWaves][kCols];
   __shared__ float red[kWaves];
+  __shared__ uint16_t list[kRanked ? kRouteThreads / kL : 1][16];
+  __shared__ int16_t picked[kStep * kMaxChoices];  // expert of every choice of the step
   const int E = a.num_experts, k = a.k;
-  const int lane = threadIdx.x % kL, group = threadIdx.x / kL;
-  for (int e = threadIdx.x; e <= E; e += kRouteThreads) {
-    bits[e] = 0;
+  const int lane = threadIdx.x % kL, group = threadIdx.x / kL, groups = blockDim.x / kL;
+  for (int e = threadIdx.x; e <= E; e += blockDim.x) {
+#pragma unroll
+    for (int w = 0; w < kWords; w++) bits[e][w] = 0;
     cnt[e] = 0;
   }
   float acc[kEpl];
@@ -127,61 +223,62 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
   const int64_t begin = (int64_t)blockIdx.x * part.per_block;
   const int64_t end = min(begin + part.per_block, a.tokens);
   __syncthreads();
-  for (int64_t first = begin; first < end; first += kGroups) {
-    const int64_t t = first + group;
-    const bool inside = t < end;
-    const bool take = inside && (!a.mask || a.mask[t]);
-    TokenRow<kL, kEpl> x;
-    x.load((const T *)a.logits + t * a.logits_stride, lane, E, take);
-    x.softmax();
+  for (int64_t first = begin; first < end; first += kStep) {
+    const int n = (int)min((int64_t)kStep, end - first);  // tokens of the step
+    for (int tile = 0; tile < n; tile += groups) {
+      const int at = tile + group;
+      const int64_t t = first + at;
+      const bool inside = at < n;
+      const bool take = inside && (!a.mask || a.mask[t]);
+      const T *row = (const T *)a.logits + t * a.logits_stride;
+      TokenRow<kL, kEpl> x;
+      x.load(row, lane, E, take);
+      x.softmax();
 #pragma unroll
-    for (int i = 0; i < kEpl; i++) acc[i] += x.p[i] * x.inv;
-    // the k largest, one at a time; lane j keeps choice j
-    int expert = -1;
-    float weight = 0;
-    for (int j = 0; j < k; j++) {
-      float m = -__builtin_inff();
-#pragma unroll
-      for (int i = 0; i < kEpl; i++) m = fmaxf(m, x.v[i]);
-      m = lanes_max<kL>(m);
-      uint32_t at = 0xFFFFFFFFu;
-#pragma unroll
-      for (int i = kEpl - 1; i >= 0; i--) at = x.v[i] == m ? (uint32_t)(lane * kEpl + i) : at;
-      at = lanes_min<kL>(at);
-      if (m == -__builtin_inff()) at = 0xFFFFFFFFu;
-#pragma unroll
-      for (int i = 0; i < kEpl; i++)
-        x.v[i] = at == (uint32_t)(lane * kEpl + i) ? -__builtin_inff() : x.v[i];
-      if (lane == j && at != 0xFFFFFFFFu) {
-        expert = (int)at;
-        weight = __expf(m - x.base);
+      for (int i = 0; i < kEpl; i++) acc[i] += x.p[i] * x.inv;
+      Choice c;
+      if (!kRanked || !choose_ranked<T, kEpl>(x.v, k, lane, row, list[group], c))
+        c = choose_each<kL, kEpl>(x.v, k, lane);
+      const int expert = c.rank < k ? c.expert : -1;
+      float weight = expert >= 0 ? __expf(c.logit - x.base) : 0.0f;
+      if (a.renorm) {
+        const float s = lanes_sum<kL>(weight);
+        weight = s == 0.0f ? 0.0f : weight / s;
+      } else {
+        weight *= x.inv;
+      }
+      const unsigned long long bit = 1ull << (at & 63);
+      if (expert >= 0) atomicOr((unsigned long long *)&bits[expert][at >> 6], bit);
+      if (lane == 0 && x.inv != 0.0f) atomicOr((unsigned long long *)&bits[E][at >> 6], bit);
+      if (inside && c.rank < k) {
+        a.experts[t * k + c.rank] = expert;
+        a.weights[t * k + c.rank] = weight;
+        picked[at * k + c.rank] = (int16_t)expert;
       }
     }
-    if (a.renorm) {
-      const float s = lanes_sum<kL>(weight);
-      weight = s == 0.0f ? 0.0f : weight / s;
-    } else {
-      weight *= x.inv;
-    }
-    if (lane < k && expert >= 0) atomicOr((unsigned long long *)&bits[expert], 1ull << group);
-    if (lane == 0 && x.inv != 0.0f) atomicOr((unsigned long long *)&bits[E], 1ull << group);
     __syncthreads();
-    if (inside && lane < k) {
-      const int64_t o = t * k + lane;
+    for (int i = threadIdx.x; i < n * k; i += blockDim.x) {
+      const int e = picked[i], at = i / k;
       int slot = -1;
-      if (expert >= 0) {
-        const uint32_t place =
-            cnt[expert] + (uint32_t)__popcll(bits[expert] & ((1ull << group) - 1));
+      if (e >= 0) {
+        uint32_t place = cnt[e];
+#pragma unroll
+        for (int w = 0; w < kWords; w++) {
+          const int past = at - 64 * w;  // bits of this word below the token's
+          const uint64_t below = past >= 64 ? ~0ull : past > 0 ? (1ull << past) - 1 : 0ull;
+          place += (uint32_t)__popcll(bits[e][w] & below);
+        }
         slot = part.blocks > 1 || !a.capacity || place < a.capacity ? (int)place : -1;
       }
-      a.experts[o] = expert;
-      a.weights[o] = weight;
-      a.slots[o] = slot;
+      a.slots[first * k + i] = slot;
     }
     __syncthreads();
-    for (int e = threadIdx.x; e <= E; e += kRouteThreads) {
-      cnt[e] += (uint32_t)__popcll(bits[e]);
-      bits[e] = 0;
+    for (int e = threadIdx.x; e <= E; e += blockDim.x) {
+#pragma unroll
+      for (int w = 0; w < kWords; w++) {
+        cnt[e] += (uint32_t)__popcll(bits[e][w]);
+        bits[e][w] = 0;
+      }
     }
     __syncthreads();
   }
@@ -198,67 +295,111 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
     for (int i = 0; i < kEpl; i++) sums[threadIdx.x >> 6][lane * kEpl + i] = acc[i];
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < E; e += kRouteThreads) {
+  const int waves = blockDim.x >> 6;
+  for (int e = threadIdx.x; e < kCols; e += blockDim.x) {
     float s = sums[0][e];
-    for (int w = 1; w < kWaves; w++) s += sums[w][e];
-    if (part.blocks > 1) part.sums[(int64_t)blockIdx.x * E + e] = s;
-    else sums[0][e] = s;
+    for (int w = 1; w < waves; w++) s += sums[w][e];
+    if (part.blocks == 1) {
+      sums[0][e] = s;
+    } else if (e < part.wide) {
+      part.sums[(int64_t)blockIdx.x * part.wide + e] = s;
+      part.counts[(int64_t)blockIdx.x * part.wide + e] = e < E ? (uint16_t)cnt[e] : 0;
+    }
   }
   if (part.blocks > 1) {
-    for (int e = threadIdx.x; e <= E; e += kRouteThreads)
-      part.counts[(int64_t)blockIdx.x * (E + 1) + e] = cnt[e];
+    if (threadIdx.x == 0) part.rows[blockIdx.x] = cnt[E];
     return;
   }
   __syncthreads();
-  finish_loss(a, cnt, sums[0], red);
+  finish_loss(a, cnt, sums[0], cnt[E], red);
 }
 
+// Column sums of n rows of `wide` values by all threads: a thread takes a
+// vector of columns of every so many rows. add() reads them, kLoads rows at a
+// time; finish() sums the threads' parts into `out` in LDS. `lds`:
+// kRouteThreads vectors.
+template <class V, int kN, class S, int kLoads>
+struct ColumnSums {
+  typedef V Vk __attribute__((ext_vector_type(kN)));
+  typedef S Sk __attribute__((ext_vector_type(kN)));
+  int wide, parts, slices;
+  Sk s;
+
+  __device__ __forceinline__ void add(const V *from, int n, int w) {
+    wide = w;
+    parts = w / kN;  // vectors per row, at most 256
+    slices = kRouteThreads / parts;
+    const int slice = threadIdx.x / parts;
+#pragma unroll
+    for (int c = 0; c < kN; c++) s[c] = 0;
+    if (slice >= slices) return;
+    const Vk *p = (const Vk *)from + threadIdx.x % parts;
+    for (int i = slice; i < n; i += kLoads * slices) {
+      Vk x[kLoads];
+#pragma unroll
+      for (int j = 0; j < kLoads; j++) x[j] = p[(int64_t)min(i + j * slices, n - 1) * parts];
+#pragma unroll
+      for (int j = 0; j < kLoads; j++)
+        if (i + j * slices < n) s += __builtin_convertvector(x[j], Sk);
+    }
+  }
+  __device__ __forceinline__ void finish(S *lds, S *out) {
+    if ((int)threadIdx.x < parts * slices) ((Sk *)lds)[threadIdx.x] = s;
+    __syncthreads();
+    for (int e = threadIdx.x; e < wide; e += kRouteThreads) {
+      S t = 0;
+      for (int i = 0; i < slices; i++) t += lds[i * wide + e];
+      out[e] = t;
+    }
+    __syncthreads();
+  }
+};
+
 // Second launch: block b adds the counts of the blocks before b to the
-// places of b's choices; the block behind them finishes the totals.
+// places of b's choices; the block behind them finishes the totals. Each
+// loads what it needs at once: a round trip to memory is the larger part of
+// its time.
 __global__ __launch_bounds__(kRouteThreads) void route_places_kernel(taccl_route_t a,
                                                                      RoutePartial part) {
-  __shared__ uint32_t cnt[kMaxExperts + 1];
+  __shared__ __align__(16) uint32_t lds[8 * kRouteThreads];
+  __shared__ uint32_t cnt[kMaxExperts];
   __shared__ float sums[kMaxExperts];
-  __shared__ float fsum[kRouteThreads];
   __shared__ float red[kRouteThreads / 64];
-  const int E = a.num_experts, b = blockIdx.x;
-  for (int e = threadIdx.x; e <= E; e += kRouteThreads) cnt[e] = 0;
-  __syncthreads();
-  // `slices` threads per expert
-  int wide = 64;
-  while (wide < E + 1 && wide < kRouteThreads) wide *= 2;
-  const int slices = kRouteThreads / wide, slice = threadIdx.x / wide;
-  for (int e = threadIdx.x % wide; e <= E; e += wide) {
-    uint32_t n = 0;
-    for (int i = slice; i < b; i += slices) n += part.counts[(int64_t)i * (E + 1) + e];
-    if (n) atomicAdd(&cnt[e], n);
-  }
-  if (b < part.blocks) {
+  const int b = blockIdx.x;
+  ColumnSums<uint16_t, 8, uint32_t, 8> counts;
+  if (b == part.blocks) {
+    ColumnSums<float, 4, float, 16> probs;
+    uint32_t n = threadIdx.x < part.blocks ? part.rows[threadIdx.x] : 0;
+    probs.add(part.sums, part.blocks, part.wide);
+    counts.add(part.counts, b, part.wide);
+    counts.finish(lds, cnt);
+    probs.finish((float *)lds, sums);
+    n = wave_scan_add(n);
+    if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = n;
     __syncthreads();
-    const int64_t begin = (int64_t)b * part.per_block;
-    const int64_t end = min(begin + part.per_block, a.tokens);
-    for (int64_t i = begin * a.k + threadIdx.x; i < end * a.k; i += kRouteThreads) {
-      const int e = a.experts[i];
-      if (e < 0) continue;
-      const uint32_t place = (uint32_t)a.slots[i] + cnt[e];
-      a.slots[i] = !a.capacity || place < a.capacity ? (int32_t)place : -1;
-    }
+    n = 0;
+    for (int w = 0; w < kRouteThreads / 64; w++) n += lds[w];
+    finish_loss(a, cnt, sums, n, red);
     return;
   }
-  for (int e0 = 0; e0 < E; e0 += wide) {
-    const int e = e0 + threadIdx.x % wide;
-    float s = 0;
-    if (e < E)
-      for (int i = slice; i < part.blocks; i += slices) s += part.sums[(int64_t)i * E + e];
-    fsum[threadIdx.x] = s;
-    __syncthreads();
-    if (slice == 0 && e < E) {
-      for (int i = 1; i < slices; i++) s += fsum[threadIdx.x + i * wide];
-      sums[e] = s;
+  const int64_t begin = (int64_t)b * part.per_block * a.k;
+  const int64_t end = min(begin + (int64_t)part.per_block * a.k, a.tokens * a.k);
+  int64_t i = begin + threadIdx.x;
+  int e = i < end ? a.experts[i] : -1;
+  int local = i < end ? a.slots[i] : 0;
+  counts.add(part.counts, b, part.wide);
+  counts.finish(lds, cnt);
+  while (i < end) {
+    if (e >= 0) {
+      const uint32_t place = (uint32_t)local + cnt[e];
+      a.slots[i] = !a.capacity || place < a.capacity ? (int32_t)place : -1;
     }
-    __syncthreads();
+    i += kRouteThreads;
+    if (i < end) {
+      e = a.experts[i];
+      local = a.slots[i];
+    }
   }
-  finish_loss(a, cnt, sums, red);
 }
 
 // Gradient: one token per group of lanes at a time. The chosen experts'
@@ -354,52 +495,63 @@ __global__ __launch_bounds__(kBackThreads) void route_backward_kernel(taccl_rout
 }
 
 // lanes per token and experts per lane: 16 lanes up to 256 experts
-template <class T, bool kBack>
-const void *route_fn(int E, int &lanes) {
-  lanes = E <= 256 ? 16 : 64;
-#define PICK(L, EPL) \
-  (kBack ? (const void *)route_backward_kernel<T, L, EPL> : (const void *)route_kernel<T, L, EPL>)
-  if (E <= 16) return PICK(16, 1);
-  if (E <= 32) return PICK(16, 2);
-  if (E <= 64) return PICK(16, 4);
-  if (E <= 128) return PICK(16, 8);
-  if (E <= 256) return PICK(16, 16);
-  if (E <= 512) return PICK(64, 8);
-  return PICK(64, 16);
-#undef PICK
-}
+#define BY_EXPERTS(E, F)                                                                   \
+  ((E) <= 16 ? F(16, 1) : (E) <= 32 ? F(16, 2) : (E) <= 64 ? F(16, 4) : (E) <= 128 ? F(16, 8) \
+   : (E) <= 256 ? F(16, 16) : (E) <= 512 ? F(64, 8) : F(64, 16))
+int token_lanes(int E) { return E <= 256 ? 16 : 64; }
 
-template <bool kBack>
-const void *route_pick(int dtype, int E, int &lanes) {
-  if (dtype == TACCL_F32) return route_fn<float, kBack>(E, lanes);
-  if (dtype == TACCL_BF16) return route_fn<bf16_t, kBack>(E, lanes);
-  return route_fn<f16_t, kBack>(E, lanes);
+template <class T>
+const void *route_fn(int E, int k) {
+  // up to 16 experts the lanes' logits are ranked as they are
+  const bool ranked = E <= 256 && (k <= 8 || E <= 16);
+#define F(L, EPL)                                                              \
+  (L == 16 && ranked ? (const void *)route_kernel<T, L, EPL, L == 16>          \
+                     : (const void *)route_kernel<T, L, EPL, false>)
+  return BY_EXPERTS(E, F);
+#undef F
+}
+template <class T>
+const void *route_backward_fn(int E) {
+#define F(L, EPL) (const void *)route_backward_kernel<T, L, EPL>
+  return BY_EXPERTS(E, F);
+#undef F
 }
 
 }  // namespace
 
 hipError_t launch_route(const taccl_route_t &a, hipStream_t stream) {
-  int lanes;
-  const void *fn = route_pick<false>(a.dtype, a.num_experts, lanes);
-  const int64_t tile = kRouteThreads / lanes;
-  RoutePartial part;
+  const int E = a.num_experts;
+  const void *fn = a.dtype == TACCL_F32    ? route_fn<float>(E, a.k)
+                   : a.dtype == TACCL_BF16 ? route_fn<bf16_t>(E, a.k)
+                                           : route_fn<f16_t>(E, a.k);
+  // small blocks spread few tokens over the CUs
+  const int threads = a.tokens <= kSmallTile || (a.tokens > kOneBlock && a.tokens <= kSmallBlocks)
+                          ? 256
+                          : kRouteThreads;
+  const int64_t tile = threads / token_lanes(E);
   const int64_t tiles = (a.tokens + tile - 1) / tile;
+  RoutePartial part;
+  part.wide = (E + 7) / 8 * 8;
   part.per_block =
       (int)(tile * std::max<int64_t>(1, (tiles + kRouteMaxBlocks - 1) / kRouteMaxBlocks));
+  if (a.tokens <= kOneBlock) part.per_block = kOneBlock;
   part.blocks = (int)std::max<int64_t>(1, (a.tokens + part.per_block - 1) / part.per_block);
-  part.counts = (uint32_t *)a.workspace;
-  part.sums = (float *)(part.counts + (int64_t)kRouteMaxBlocks * (a.num_experts + 1));
+  part.sums = (float *)a.workspace;
+  part.rows = (uint32_t *)(part.sums + (int64_t)kRouteMaxBlocks * part.wide);
+  part.counts = (uint16_t *)(part.rows + kRouteMaxBlocks);
   void *args[] = {(void *)&a, &part};
-  hipError_t e = hipLaunchKernel(fn, dim3(part.blocks), dim3(kRouteThreads), args, 0, stream);
+  hipError_t e = hipLaunchKernel(fn, dim3(part.blocks), dim3(threads), args, 0, stream);
   if (e != hipSuccess || part.blocks == 1) return e;
   return hipLaunchKernel((const void *)route_places_kernel, dim3(part.blocks + 1),
                          dim3(kRouteThreads), args, 0, stream);
 }
 
 hipError_t launch_route_backward(const taccl_route_backward_t &a, int cus, hipStream_t stream) {
-  int lanes;
-  const void *fn = route_pick<true>(a.dtype, a.num_experts, lanes);
-  const int groups = kBackThreads / lanes;
+  const int E = a.num_experts;
+  const void *fn = a.dtype == TACCL_F32    ? route_backward_fn<float>(E)
+                   : a.dtype == TACCL_BF16 ? route_backward_fn<bf16_t>(E)
+                                           : route_backward_fn<f16_t>(E);
+  const int groups = kBackThreads / token_lanes(E);
   const int grid =
       (int)std::min<int64_t>((a.tokens + groups - 1) / groups, (int64_t)std::max(cus, 1) * 8);
   void *args[] = {(void *)&a};
