@@ -106,7 +106,7 @@ __device__ __forceinline__ float dppf(float v) {
 constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
 constexpr int kRor8 = 0x128, kRor4 = 0x124, kRor2 = 0x122, kRor1 = 0x121;
 
-// Sums and maxima over groups of L lanes (16: one DPP row, 64: the
+// Sums and maxima over groups of L lanes (16: one DPP row; 32; 64: the
 // wavefront), the same in every lane of the group. Sums go down a fixed tree.
 template <int L>
 __device__ __forceinline__ float lanes_sum(float v) {
@@ -114,10 +114,8 @@ __device__ __forceinline__ float lanes_sum(float v) {
   v += dppf<kRor4>(v);
   v += dppf<kRor2>(v);
   v += dppf<kRor1>(v);
-  if (L == 64) {
-    v += __shfl_xor(v, 16);
-    v += __shfl_xor(v, 32);
-  }
+  if (L >= 32) v += __shfl_xor(v, 16);
+  if (L == 64) v += __shfl_xor(v, 32);
   return v;
 }
 template <int L>
