@@ -1,6 +1,7 @@
 // C ABI of the expert-layer operators: checks of arguments and launches.
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <string>
 
 #include "expert.h"
@@ -70,13 +71,16 @@ taccl_status_t launched(hipError_t e, const char *call) {
   return fail(TACCL_ERR_HIP, std::string(call) + ": kernel launch: " + hipGetErrorString(e));
 }
 
-// CUs of the current device
+// CUs of the current device (asked for once per device)
 taccl_status_t device_cus(const char *call, int *cus) {
+  static std::atomic<int> known[64];
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
+  if (e == hipSuccess && dev >= 0 && dev < 64 && (*cus = known[dev].load()) > 0) return TACCL_OK;
   if (e == hipSuccess) e = hipDeviceGetAttribute(cus, hipDeviceAttributeMultiprocessorCount, dev);
   if (e != hipSuccess)
     return fail(TACCL_ERR_HIP, std::string(call) + ": " + hipGetErrorString(e));
+  if (dev < 64) known[dev].store(*cus);
   return TACCL_OK;
 }
 

@@ -7,8 +7,7 @@
 //   renormalised (w = softmax over the chosen logits):
 //   dl_{e_j} += w_j (dw_j - sum_i w_i dw_i)
 //
-// A group of kL lanes holds one token's logits, kEpl consecutive experts per
-// lane. The sums over tokens go through per-block partial results and a
+// A group of kL lanes holds one token's logits, kEpl experts per lane. The sums over tokens go through per-block partial results and a
 // second launch, never through floating atomics, so their order is fixed.
 #include <hip/hip_runtime.h>
 
@@ -36,44 +35,62 @@ struct RoutePartial {
   int blocks;
 };
 
-// One token's logits in a group of lanes: softmax statistics.
-template <int kL, int kEpl>
+// One token's logits in a group of kL lanes. The experts are dealt out in
+// vectors of kN, one to each lane in turn, so that a group reads one piece of
+// memory at a time; element i of a lane is expert index(lane, i), which grows
+// with i.
+template <class T, int kL, int kEpl>
 struct TokenRow {
-  float v[kEpl];  // minus infinity past the experts and in rows not taken
+  static constexpr int kN = Vec<T>::kN < kEpl ? Vec<T>::kN : kEpl;
+  static constexpr int kSlots = kEpl / kN;
+  typedef T W __attribute__((ext_vector_type(kN)));
+  typedef W U __attribute__((aligned(sizeof(T))));
+  static __device__ __forceinline__ int index(int lane, int i) {
+    return lane * kN + i / kN * (kL * kN) + i % kN;
+  }
 
-  template <class T>
+  float v[kEpl];  // minus infinity past the experts and in rows not taken
   __device__ __forceinline__ void load(const T *row, int lane, int E, bool take) {
-    constexpr int N = Vec<T>::kN < kEpl ? Vec<T>::kN : kEpl;
-    const int first = lane * kEpl;
+    if (take && E == kL * kEpl) {
+#pragma unroll
+      for (int s = 0; s < kSlots; s++) {
+        const W w = *(const U *)(row + index(lane, s * kN));
+#pragma unroll
+        for (int x = 0; x < kN; x++) v[s * kN + x] = (float)w[x];
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < kEpl; i++) v[i] = -__builtin_inff();
     if (!take) return;
-    if (first + kEpl <= E) {
-      typedef T W __attribute__((ext_vector_type(N)));
-      typedef W U __attribute__((aligned(sizeof(T))));
 #pragma unroll
-      for (int i = 0; i < kEpl; i += N) {
-        const W w = *(const U *)(row + first + i);
+    for (int s = 0; s < kSlots; s++) {
+      const int e = index(lane, s * kN);
+      if (e + kN <= E) {
+        const W w = *(const U *)(row + e);
 #pragma unroll
-        for (int x = 0; x < N; x++) v[i + x] = (float)w[x];
+        for (int x = 0; x < kN; x++) v[s * kN + x] = (float)w[x];
+      } else {
+#pragma unroll
+        for (int x = 0; x < kN; x++)
+          if (e + x < E) v[s * kN + x] = (float)row[e + x];
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kEpl; i++)
-        if (first + i < E) v[i] = (float)row[first + i];
     }
   }
 
-  // the exponent's offset (0 in a row of minus infinities and NaNs), the
-  // exponentials and 1 / their sum, 0 in a row without a number
-  float base, inv;
+  // Softmax: the lane's maximum and the exponent's offset (0 in a row of minus
+  // infinities and NaNs); the exponentials and 1 / their sum, 0 in a row
+  // without a number.
+  float top, base, inv;
   float p[kEpl];  // exp(v - base)
-  __device__ __forceinline__ void softmax() {
-    float m = -__builtin_inff();
+  __device__ __forceinline__ void maxima() {
+    top = -__builtin_inff();
 #pragma unroll
-    for (int i = 0; i < kEpl; i++) m = fmaxf(m, v[i]);
-    m = lanes_max<kL>(m);
+    for (int i = 0; i < kEpl; i++) top = fmaxf(top, v[i]);
+    const float m = lanes_max<kL>(top);
     base = m == -__builtin_inff() ? 0.0f : m;
+  }
+  __device__ __forceinline__ void exponentials() {
     float s = 0;
 #pragma unroll
     for (int i = 0; i < kEpl; i++) {
@@ -81,20 +98,10 @@ struct TokenRow {
       s += p[i];
     }
     s = lanes_sum<kL>(s);
-    inv = s == 0.0f ? 0.0f : 1.0f / s;
+    inv = s == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(s);  // within one unit in the last place
   }
 };
 
-// Rank (0 = largest) of `key` in its row of 16 lanes, equal keys by lane
-__device__ __forceinline__ int row_rank(int key, int lane) {
-  int rank = 0;
-#define BEATEN(R) \
-  rank += (int)dpp<0x120 + R>((uint32_t)key) > (lane >= R ? key - 1 : key) ? 1 : 0;
-  BEATEN(1) BEATEN(2) BEATEN(3) BEATEN(4) BEATEN(5) BEATEN(6) BEATEN(7) BEATEN(8)
-  BEATEN(9) BEATEN(10) BEATEN(11) BEATEN(12) BEATEN(13) BEATEN(14) BEATEN(15)
-#undef BEATEN
-  return rank;
-}
 // floats as integers in the same order (both zeros alike, no NaN); kNone is
 // below minus infinity's
 constexpr int kNone = -0x7FFFFFFF;
@@ -103,29 +110,88 @@ __device__ __forceinline__ int order_key(float v) {
   return x ^ ((x >> 31) & 0x7FFFFFFF);
 }
 
+#define IN_ROW(F) \
+  F(1) F(2) F(3) F(4) F(5) F(6) F(7) F(8) F(9) F(10) F(11) F(12) F(13) F(14) F(15)
+
+// Rank (0 = largest) of a lane's candidate in its row of 16 lanes, equal
+// logits in the order of their expert; `n` candidates in the row, in lanes 0 to
+// n - 1 of it. A 16-bit logit and the expert make one key; 32-bit ones are
+// equal so seldom that the experts are compared only then.
+template <class T>
+__device__ __forceinline__ int row_rank(bool there, float logit, int expert, uint32_t n) {
+  int key;
+  if constexpr (sizeof(T) == 2) {
+    const int x = __builtin_bit_cast(int16_t, (T)(logit + 0.0f));
+    key = (int)((uint32_t)(x ^ ((x >> 15) & 0x7FFF)) << 16 | (0xFFFFu - (uint32_t)expert));
+  } else {
+    key = order_key(logit);
+  }
+  if (!there) key = kNone;
+  uint32_t rank = 0;
+#define BEATEN(R) rank += (int)dpp<0x120 + R>((uint32_t)key) > key ? 1u : 0u;
+  IN_ROW(BEATEN)
+#undef BEATEN
+  if (sizeof(T) == 2) return (int)rank;
+  uint32_t taken = there ? 1u << rank : 0u;
+  taken |= dpp<kRor8>(taken);
+  taken |= dpp<kRor4>(taken);
+  taken |= dpp<kRor2>(taken);
+  taken |= dpp<kRor1>(taken);
+  if (!__any(taken != (1u << n) - 1)) return (int)rank;
+#define EQUAL(R)                                        \
+  {                                                     \
+    const int k = (int)dpp<0x120 + R>((uint32_t)key);   \
+    const int x = (int)dpp<0x120 + R>((uint32_t)expert); \
+    rank += k == key && x < expert ? 1u : 0u;           \
+  }
+  IN_ROW(EQUAL)
+#undef EQUAL
+  return (int)rank;
+}
+
+// The row's values in descending order (bitonic merges over mirrored halves)
+__device__ __forceinline__ float row_sorted(float v, int lane) {
+  auto step = [&](float o, int bit) {
+    const float hi = fmaxf(v, o), lo = fminf(v, o);
+    v = lane & bit ? lo : hi;
+  };
+  constexpr int kMirror4 = 0x1B;  // quad_perm [3, 2, 1, 0]
+  step(dppf<kXor1>(v), 1);
+  step(dppf<kMirror4>(v), 2);
+  step(dppf<kXor1>(v), 1);
+  step(dppf<kHalfMirror>(v), 4);
+  step(dppf<kXor2>(v), 2);
+  step(dppf<kXor1>(v), 1);
+  step(dppf<kMirror>(v), 8);
+  step(dppf<kMirror4>(dppf<kHalfMirror>(v)), 4);
+  step(dppf<kXor2>(v), 2);
+  step(dppf<kXor1>(v), 1);
+  return v;
+}
+
 // A lane's choice: rank among the token's choices, expert (-1: none) and logit
 struct Choice {
   int rank, expert;
   float logit;
 };
 
-// One at a time: the row's maximum k times. Changes v.
-template <int kL, int kEpl>
-__device__ __forceinline__ Choice choose_each(float *v, int k, int lane) {
+// One at a time: the row's maximum k times. Changes x.v.
+template <class T, int kL, int kEpl>
+__device__ __forceinline__ Choice choose_each(TokenRow<T, kL, kEpl> &x, int k, int lane) {
   Choice c{lane, -1, 0.0f};
   for (int j = 0; j < k; j++) {
     float m = -__builtin_inff();
 #pragma unroll
-    for (int i = 0; i < kEpl; i++) m = fmaxf(m, v[i]);
+    for (int i = 0; i < kEpl; i++) m = fmaxf(m, x.v[i]);
     m = lanes_max<kL>(m);
     uint32_t at = 0xFFFFFFFFu;
 #pragma unroll
-    for (int i = kEpl - 1; i >= 0; i--) at = v[i] == m ? (uint32_t)(lane * kEpl + i) : at;
+    for (int i = kEpl - 1; i >= 0; i--) at = x.v[i] == m ? (uint32_t)x.index(lane, i) : at;
     at = lanes_min<kL>(at);
     if (m == -__builtin_inff()) at = 0xFFFFFFFFu;
 #pragma unroll
     for (int i = 0; i < kEpl; i++)
-      v[i] = at == (uint32_t)(lane * kEpl + i) ? -__builtin_inff() : v[i];
+      x.v[i] = at == (uint32_t)x.index(lane, i) ? -__builtin_inff() : x.v[i];
     if (lane == j && at != 0xFFFFFFFFu) {
       c.expert = (int)at;
       c.logit = m;
@@ -134,43 +200,78 @@ __device__ __forceinline__ Choice choose_each(float *v, int k, int lane) {
   return c;
 }
 
-// By a threshold: the k-th largest of the 16 lanes' maxima bounds the k-th
+// By a threshold: the k-th largest of the lanes' maxima bounds the k-th
 // largest logit from below, so the choices are among the logits that reach it.
-// Where at most 16 do (for k = 8 about 11 of 256 random ones), one lane takes
-// each, in the order of their index, and their ranks are the choice. False:
-// some row of the wavefront has more.
-template <class T, int kEpl>
-__device__ __forceinline__ bool choose_ranked(const float *v, int k, int lane, const T *row,
-                                              uint16_t *list, Choice &c) {
-  float m = -__builtin_inff();
-#pragma unroll
-  for (int i = 0; i < kEpl; i++) m = fmaxf(m, v[i]);
-  const int top = row_rank(order_key(m), lane);
+// Where at most 16 do (for k = 8 about 10 of 256 random ones, 0.7% of the rows
+// have more), lanes 0 to 15 of the group take one each, and their ranks are
+// the choice. list_ranked() finds the candidates and has their
+// logits loaded again (a lane's element is no register index), to be used
+// behind the exponentials by rank_listed(). False: some row of the wavefront
+// has more.
+template <class T, int kL, int kEpl>
+__device__ __forceinline__ bool list_ranked(const TokenRow<T, kL, kEpl> &x, int k, int lane,
+                                            const T *row, uint16_t *list, Choice &c,
+                                            uint32_t &n) {
+  typedef TokenRow<T, kL, kEpl> Row;
   // at least the lowest number: minus infinities are never chosen
-  const float bound = lanes_max<16>(top == k - 1 ? fmaxf(m, -__FLT_MAX__) : -__FLT_MAX__);
+  float bound = -__FLT_MAX__;
+  if (kL == 16) {
+    const float sorted = fmaxf(row_sorted(x.top, lane), bound);  // by every lane of the row
+    bound = lanes_max<16>(lane == k - 1 ? sorted : bound);
+  } else {
+    float m = x.top, most = m;
+    for (int j = 0; j < k; j++) {  // the lanes' maxima, one lane after the other
+      most = lanes_max<64>(m);
+      const uint64_t same = __ballot(m == most);
+      if (same && lane == __ffsll((unsigned long long)same) - 1) m = -__builtin_inff();
+    }
+    bound = fmaxf(most, bound);
+  }
   uint32_t hit = 0;
 #pragma unroll
-  for (int i = 0; i < kEpl; i++)
-    hit |= v[i] >= bound ? 1u << i : 0u;
-  const uint32_t mine = __popc(hit), upto = row_scan_add(mine);
-  const uint32_t all = dpp<0x15F>(upto);  // the row's last lane
+  for (int i = 0; i < kEpl; i++) hit |= x.v[i] >= bound ? 1u << i : 0u;
+  const uint32_t mine = __popc(hit);
+  const uint32_t upto = kL == 16 ? row_scan_add(mine) : wave_scan_add(mine);
+  const uint32_t all = kL == 16 ? dpp<0x15F>(upto)  // the row's last lane
+                                : (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
   if (__any(all > 16)) return false;
-  for (uint32_t at = upto - mine; __any(hit); hit &= hit - 1, at++)
-    if (hit) list[at] = (uint16_t)(lane * kEpl + __ffs(hit) - 1);
+  uint32_t at = upto - mine;
+  do {  // a lane without a further one writes past the list
+    const int i = __ffs(hit) - 1;
+    list[hit ? at : 16] = (uint16_t)Row::index(lane, i);
+    hit &= hit - 1;
+    at++;
+  } while (__any(hit));
   __builtin_amdgcn_wave_barrier();
   asm volatile("" ::: "memory");  // one wavefront's LDS accesses are in order
+  n = all;
   c = Choice{lane, -1, 0.0f};
-  int key = kNone;
   if ((uint32_t)lane < all) {
     c.expert = list[lane];
     c.logit = (float)row[c.expert];
-    key = order_key(c.logit);
   }
-  const int rank = row_rank(key, lane);
-  if ((uint32_t)lane < all) c.rank = rank;
   __builtin_amdgcn_wave_barrier();
   asm volatile("" ::: "memory");
   return true;
+}
+template <class T>
+__device__ __forceinline__ void rank_listed(Choice &c, uint32_t n, int lane) {
+  const int rank = row_rank<T>(c.expert >= 0, c.logit, c.expert, lane < 16 ? n : 0);
+  if (c.expert >= 0) c.rank = rank;
+}
+
+// Sums over the wavefront's four rows of 16 lanes, one of four values to each
+// row: the total of v[0], v[2], v[1], v[3] in rows 0 to 3. A swap puts half of
+// two registers into one, so two values are added with one addition.
+__device__ __forceinline__ float rows_sum(const float *v) {
+  auto pair = [](float a, float b, bool rows) {
+    const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+    const auto r = rows ? __builtin_amdgcn_permlane16_swap(x, y, false, false)
+                        : __builtin_amdgcn_permlane32_swap(x, y, false, false);
+    const uint32_t first = r[0], second = r[1];
+    return __uint_as_float(first) + __uint_as_float(second);
+  };
+  return pair(pair(v[0], v[1], false), pair(v[2], v[3], false), true);
 }
 
 // The balance loss and the totals from the experts' counts and sums in LDS
@@ -208,7 +309,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
   __shared__ uint32_t cnt[kCols + 1];
   __shared__ float sums[kWaves][kCols];
   __shared__ float red[kWaves];
-  __shared__ uint16_t list[kRanked ? kRouteThreads / kL : 1][16];
+  __shared__ uint16_t list[kRanked ? kRouteThreads / kL : 1][16 + 1];
   __shared__ int16_t picked[kStep * kMaxChoices];  // expert of every choice of the step
   const int E = a.num_experts, k = a.k;
   const int lane = threadIdx.x % kL, group = threadIdx.x / kL, groups = blockDim.x / kL;
@@ -231,19 +332,22 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
       const bool inside = at < n;
       const bool take = inside && (!a.mask || a.mask[t]);
       const T *row = (const T *)a.logits + t * a.logits_stride;
-      TokenRow<kL, kEpl> x;
+      TokenRow<T, kL, kEpl> x;
       x.load(row, lane, E, take);
-      x.softmax();
+      x.maxima();
+      Choice c;
+      uint32_t n_listed = 0;
+      const bool listed = kRanked && list_ranked(x, k, lane, row, list[group], c, n_listed);
+      x.exponentials();
 #pragma unroll
       for (int i = 0; i < kEpl; i++) acc[i] += x.p[i] * x.inv;
-      Choice c;
-      if (!kRanked || !choose_ranked<T, kEpl>(x.v, k, lane, row, list[group], c))
-        c = choose_each<kL, kEpl>(x.v, k, lane);
+      if (listed) rank_listed<T>(c, n_listed, lane);
+      else c = choose_each(x, k, lane);
       const int expert = c.rank < k ? c.expert : -1;
       float weight = expert >= 0 ? __expf(c.logit - x.base) : 0.0f;
       if (a.renorm) {
         const float s = lanes_sum<kL>(weight);
-        weight = s == 0.0f ? 0.0f : weight / s;
+        weight *= s == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(s);
       } else {
         weight *= x.inv;
       }
@@ -282,17 +386,22 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
     }
     __syncthreads();
   }
-  // the block's probability sums: groups of a wavefront, then wavefronts
-  if (kL == 16) {
+  // the block's probability sums: rows of a wavefront, then wavefronts
+  float *mine = sums[threadIdx.x >> 6];
+  typedef TokenRow<T, kL, kEpl> Row;
+  if (kL == 64) {
 #pragma unroll
-    for (int i = 0; i < kEpl; i++) {
-      acc[i] += __shfl_xor(acc[i], 16);
-      acc[i] += __shfl_xor(acc[i], 32);
+    for (int i = 0; i < kEpl; i++) mine[Row::index(lane, i)] = acc[i];
+  } else {
+    const int r = (threadIdx.x & 63) >> 4, turn = (r >> 1) | (r & 1) << 1;  // rows_sum's order
+#pragma unroll
+    for (int i = 0; i < kEpl; i += 4) {
+      float v[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < 4 && i + j < kEpl; j++) v[j] = acc[i + j];
+      const float s = rows_sum(v);
+      if (i + turn < kEpl) mine[Row::index(lane, i) + turn] = s;
     }
-  }
-  if ((threadIdx.x & 63) < kL) {
-#pragma unroll
-    for (int i = 0; i < kEpl; i++) sums[threadIdx.x >> 6][lane * kEpl + i] = acc[i];
   }
   __syncthreads();
   const int waves = blockDim.x >> 6;
@@ -328,7 +437,7 @@ struct ColumnSums {
   __device__ __forceinline__ void add(const V *from, int n, int w) {
     wide = w;
     parts = w / kN;  // vectors per row, at most 256
-    slices = kRouteThreads / parts;
+    slices = min(kRouteThreads / parts, 32);  // finish() reads them in turn
     const int slice = threadIdx.x / parts;
 #pragma unroll
     for (int c = 0; c < kN; c++) s[c] = 0;
@@ -407,18 +516,20 @@ __global__ __launch_bounds__(kRouteThreads) void route_places_kernel(taccl_route
 // in order), zero outside them.
 template <class T, int kL, int kEpl>
 __global__ __launch_bounds__(kBackThreads) void route_backward_kernel(taccl_route_backward_t a) {
-  constexpr int kGroups = kBackThreads / kL, kCols = kL * kEpl;
-  __shared__ float chosen[kGroups][kCols];
+  typedef TokenRow<T, kL, kEpl> Row;
+  constexpr int kGroups = kBackThreads / kL, kCols = kL * kEpl, kN = Row::kN;
+  __shared__ __align__(16) float chosen[kGroups][kCols];
   const int E = a.num_experts, k = a.k;
   const int lane = threadIdx.x % kL, group = threadIdx.x / kL;
-  float *own = chosen[group] + lane * kEpl;
+  float *own = chosen[group];
   const float n = (float)max(*a.rows, 1);
   const float scale = a.dloss ? *a.dloss * a.coef * (float)E / (n * n * (float)k) : 0.0f;
   float load[kEpl];
 #pragma unroll
   for (int i = 0; i < kEpl; i++) {
-    own[i] = 0;
-    load[i] = lane * kEpl + i < E ? scale * (float)a.counts[lane * kEpl + i] : 0.0f;
+    const int e = Row::index(lane, i);
+    own[e] = 0;
+    load[i] = e < E ? scale * (float)a.counts[e] : 0.0f;
   }
   for (int64_t first = (int64_t)blockIdx.x * kGroups; first < a.tokens;
        first += (int64_t)gridDim.x * kGroups) {
@@ -426,38 +537,34 @@ __global__ __launch_bounds__(kBackThreads) void route_backward_kernel(taccl_rout
     const bool inside = t < a.tokens;
     const bool take = inside && (!a.mask || a.mask[t]);
     const T *row = (const T *)a.logits + t * a.logits_stride;
-    TokenRow<kL, kEpl> x;
-    x.load(row, lane, E, take);
     int expert = -1;
     float dw = 0, weight = 0;
-    if (a.dweights) {  // the same for every lane
-      if (take && lane < k) {
-        expert = a.experts[t * k + lane];
-        if ((uint32_t)expert < (uint32_t)E) {
-          dw = a.dweights[t * k + lane];
-          weight = (float)row[expert];
-        } else {
-          expert = -1;
-        }
-      }
+    if (a.dweights && take && lane < k) {
+      expert = a.experts[t * k + lane];
+      dw = a.dweights[t * k + lane];
     }
-    x.softmax();
+    Row x;
+    x.load(row, lane, E, take);
+    if ((uint32_t)expert < (uint32_t)E) weight = (float)row[expert];
+    else expert = -1;
+    x.maxima();
+    x.exponentials();
     if (a.dweights) {
       weight = expert >= 0 ? __expf(weight - x.base) : 0.0f;
       float term = dw;
       if (a.renorm) {
         const float s = lanes_sum<kL>(weight);
-        weight = s == 0.0f ? 0.0f : weight / s;
+        weight *= s == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(s);
         term = weight * (dw - lanes_sum<kL>(weight * dw));
       }
-      if (expert >= 0) chosen[group][expert] = term;
+      if (expert >= 0) own[expert] = term;
       __builtin_amdgcn_wave_barrier();
       asm volatile("" ::: "memory");
     }
     float c[kEpl], dot = 0;
 #pragma unroll
     for (int i = 0; i < kEpl; i++) {
-      c[i] = a.dweights ? own[i] : 0.0f;
+      c[i] = a.dweights ? own[Row::index(lane, i)] : 0.0f;
       x.p[i] *= x.inv;
       dot += x.p[i] * (a.renorm ? load[i] : load[i] + c[i]);
     }
@@ -465,31 +572,28 @@ __global__ __launch_bounds__(kBackThreads) void route_backward_kernel(taccl_rout
     if (a.dweights) {
       __builtin_amdgcn_wave_barrier();
       asm volatile("" ::: "memory");
-      if (expert >= 0) chosen[group][expert] = 0;
+      if (expert >= 0) own[expert] = 0;
     }
     if (!inside) continue;
-    T *out = (T *)a.dlogits + t * a.dlogits_stride + lane * kEpl;
-    T g[kEpl];
+    T *out = (T *)a.dlogits + t * a.dlogits_stride;
 #pragma unroll
-    for (int i = 0; i < kEpl; i++)
-      g[i] = (T)(x.inv == 0.0f ? 0.0f
-                 : a.renorm    ? x.p[i] * (load[i] - dot) + c[i]
-                               : x.p[i] * (load[i] + c[i] - dot));
-    constexpr int N = Vec<T>::kN < kEpl ? Vec<T>::kN : kEpl;
-    typedef T W __attribute__((ext_vector_type(N)));
-    typedef W U __attribute__((aligned(sizeof(T))));
-    if (lane * kEpl + kEpl <= E) {
+    for (int s = 0; s < Row::kSlots; s++) {
+      typename Row::W w;
 #pragma unroll
-      for (int i = 0; i < kEpl; i += N) {
-        W w;
-#pragma unroll
-        for (int y = 0; y < N; y++) w[y] = g[i + y];
-        *(U *)(out + i) = w;
+      for (int y = 0; y < kN; y++) {
+        const int i = s * kN + y;
+        w[y] = (T)(x.inv == 0.0f ? 0.0f
+                   : a.renorm    ? x.p[i] * (load[i] - dot) + c[i]
+                                 : x.p[i] * (load[i] + c[i] - dot));
       }
-    } else {
+      const int e = Row::index(lane, s * kN);
+      if (e + kN <= E) {
+        *(typename Row::U *)(out + e) = w;
+      } else {
 #pragma unroll
-      for (int i = 0; i < kEpl; i++)
-        if (lane * kEpl + i < E) out[i] = g[i];
+        for (int y = 0; y < kN; y++)
+          if (e + y < E) out[e + y] = w[y];
+      }
     }
   }
 }
@@ -502,11 +606,10 @@ int token_lanes(int E) { return E <= 256 ? 16 : 64; }
 
 template <class T>
 const void *route_fn(int E, int k) {
-  // up to 16 experts the lanes' logits are ranked as they are
-  const bool ranked = E <= 256 && (k <= 8 || E <= 16);
-#define F(L, EPL)                                                              \
-  (L == 16 && ranked ? (const void *)route_kernel<T, L, EPL, L == 16>          \
-                     : (const void *)route_kernel<T, L, EPL, false>)
+  const bool ranked = k <= 8 || E <= 16;
+#define F(L, EPL)                                               \
+  (ranked ? (const void *)route_kernel<T, L, EPL, true>         \
+          : (const void *)route_kernel<T, L, EPL, false>)
   return BY_EXPERTS(E, F);
 #undef F
 }

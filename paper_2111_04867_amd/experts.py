@@ -66,13 +66,18 @@ _CombineBackward = _struct("_CombineBackward", [
 _calls = {}
 
 
-def _call(name, args, stream):
-    fn = _calls.get(name)
-    if fn is None:
-        fn = getattr(binding.lib(), name)
-        fn.argtypes, fn.restype = [_P, _P], ct.c_int
-        _calls[name] = fn
-    status = fn(ct.addressof(args), binding._stream_handle(torch, stream))
+def _bind(name):
+    fn = getattr(binding.lib(), name)
+    fn.argtypes, fn.restype = [_P, _P], ct.c_int
+    _calls[name] = fn
+    return fn
+
+
+def _call(name, args, device, stream):
+    """The library's call on `stream`, or on the current one of `device`."""
+    fn = _calls.get(name) or _bind(name)
+    status = fn(ct.addressof(args), torch._C._cuda_getCurrentRawStream(device)
+                if stream is None else stream.cuda_stream)
     if status:
         binding._check(status)
 
@@ -93,38 +98,55 @@ def route_workspace(num_experts):
     return _size("taccl_route_workspace", int(num_experts))
 
 
-def _rows(t, name, shape, dtype):
-    """(pointer, row stride) of a CUDA matrix with a contiguous last axis."""
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor {list(shape)} of {dtype}, got "
-                         f"{list(t.shape)} of {t.dtype} on {t.device}")
-    row, col = t.stride()
-    if col != 1 and shape[1] > 1:
-        raise ValueError(f"{name}'s last axis must be contiguous")
-    return t.data_ptr(), row
+def _wrong(t, name, what, shape, dtype):
+    return ValueError(f"{name} must be a {what} {list(shape)} of {dtype}, got {list(t.shape)} of "
+                      f"{t.dtype} with strides {t.stride()} on {t.device}")
 
 
-def _flat(t, name, shape, dtype):
-    """Pointer of a contiguous CUDA tensor."""
-    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous CUDA tensor {list(shape)} of {dtype}, got "
-                         f"{list(t.shape)} of {t.dtype} on {t.device}")
-    return t.data_ptr()
+def _rows(t, name, shape, dtype, device):
+    """(pointer, row stride) of a matrix on `device` with a contiguous last axis."""
+    if t.dtype is dtype and t.get_device() == device and t.shape == shape:
+        stride = t.stride()
+        if stride[1] == 1 or shape[1] <= 1:
+            return t.data_ptr(), stride[0]
+    raise _wrong(t, name, "CUDA tensor with contiguous rows", shape, dtype)
 
 
-def _matrix(t, name, dtypes=_DTYPES):
-    """(shape, dtype) of the tensor that a call's others go by."""
-    if t.dim() != 2 or t.dtype not in dtypes:
-        raise ValueError(f"{name} must be a matrix of {', '.join(str(d) for d in dtypes)}, got "
-                         f"{list(t.shape)} of {t.dtype}")
-    if t.is_cuda and t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, not on the current device")
-    return t.shape, t.dtype
+def _flat(t, name, shape, dtype, device):
+    """Pointer of a contiguous tensor on `device`."""
+    if t.dtype is dtype and t.get_device() == device and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    raise _wrong(t, name, "contiguous CUDA tensor", shape, dtype)
 
 
-def _bytes(t, name):
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous CUDA tensor")
+def _on_device(t, name):
+    """Index of the tensor's device, which has to be the current one."""
+    device = t.get_device()
+    if device < 0 or device != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} must be a CUDA tensor on the current device, is on {t.device}")
+    return device
+
+
+def _matrix(t, name):
+    """(shape, type, its code, device) of the tensor that a call's others go by."""
+    dtype = t.dtype
+    code = _DTYPES.get(dtype)
+    if code is None or t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix of {', '.join(str(d) for d in _DTYPES)}, got "
+                         f"{list(t.shape)} of {dtype}")
+    return t.shape, dtype, code, _on_device(t, name)
+
+
+def _code(dtype, name):
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise ValueError(f"{name} is of {dtype}, must be one of {', '.join(map(str, _DTYPES))}")
+    return code
+
+
+def _bytes(t, name, device):
+    if t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous CUDA tensor on the current device")
     return t.data_ptr(), t.numel() * t.element_size()
 
 
@@ -136,24 +158,25 @@ def norm_tensors(x, weight, out=None, *, eps=1e-6, residual=None, total=None, q=
     total = h; q (float8_e4m3fn) = out / scale, scale [rows, ceil(cols /
     group)] in 32 bits (group 0: one column). Outputs that are None are left
     out."""
-    shape, dtype = _matrix(x, "x")
+    shape, dtype, code, device = _matrix(x, "x")
     n, d = shape
-    p, stride = _rows(x, "x", shape, dtype)
+    p, stride = _rows(x, "x", shape, dtype, device)
     r = o = h = f = s = None
     r_stride = o_stride = h_stride = f_stride = s_stride = 0
     if residual is not None:
-        r, r_stride = _rows(residual, "residual", shape, dtype)
+        r, r_stride = _rows(residual, "residual", shape, dtype, device)
     if out is not None:
-        o, o_stride = _rows(out, "out", shape, dtype)
+        o, o_stride = _rows(out, "out", shape, dtype, device)
     if total is not None:
-        h, h_stride = _rows(total, "total", shape, dtype)
+        h, h_stride = _rows(total, "total", shape, dtype, device)
     if q is not None:
-        f, f_stride = _rows(q, "q", shape, torch.float8_e4m3fn)
+        f, f_stride = _rows(q, "q", shape, torch.float8_e4m3fn, device)
     if scale is not None:
-        s, s_stride = _rows(scale, "scale", (n, -(-d // group) if group else 1), torch.float32)
-    _call("taccl_norm", _Norm(n, d, _DTYPES[dtype], eps, group, p, r, stride, r_stride,
-                              _flat(weight, "weight", (d,), dtype), o, h, o_stride, h_stride, f, s,
-                              f_stride, s_stride), stream)
+        s, s_stride = _rows(scale, "scale", (n, -(-d // group) if group else 1), torch.float32,
+                            device)
+    w = _flat(weight, "weight", (d,), dtype, device)
+    _call("taccl_norm", _Norm(n, d, code, eps, group, p, r, stride, r_stride, w, o, h, o_stride,
+                              h_stride, f, s, f_stride, s_stride), device, stream)
 
 
 def norm_backward_tensors(dout, h, weight, dx, dweight, workspace, *, eps=1e-6, dtotal=None,
@@ -161,17 +184,18 @@ def norm_backward_tensors(dout, h, weight, dx, dweight, workspace, *, eps=1e-6, 
     """taccl_norm_backward: dx (of x and of residual) and dweight (32 bits)
     from dout, the stored total h and the gradient dtotal that reaches h
     directly."""
-    shape, dtype = _matrix(h, "h")
+    shape, dtype, code, device = _matrix(h, "h")
     n, d = shape
-    g, g_stride = _rows(dout, "dout", shape, dtype)
-    p, stride = _rows(h, "h", shape, dtype)
-    t, t_stride = (None, 0) if dtotal is None else _rows(dtotal, "dtotal", shape, dtype)
-    o, o_stride = _rows(dx, "dx", shape, dtype)
-    w, w_bytes = _bytes(workspace, "workspace")
+    g, g_stride = _rows(dout, "dout", shape, dtype, device)
+    p, stride = _rows(h, "h", shape, dtype, device)
+    t, t_stride = (None, 0) if dtotal is None else _rows(dtotal, "dtotal", shape, dtype, device)
+    o, o_stride = _rows(dx, "dx", shape, dtype, device)
+    w, w_bytes = _bytes(workspace, "workspace", device)
     _call("taccl_norm_backward",
-          _NormBackward(n, d, _DTYPES[dtype], eps, g, p, t, g_stride, stride, t_stride,
-                        _flat(weight, "weight", (d,), dtype), o, o_stride,
-                        _flat(dweight, "dweight", (d,), torch.float32), w, w_bytes), stream)
+          _NormBackward(n, d, code, eps, g, p, t, g_stride, stride, t_stride,
+                        _flat(weight, "weight", (d,), dtype, device), o, o_stride,
+                        _flat(dweight, "dweight", (d,), torch.float32, device), w, w_bytes),
+          device, stream)
 
 
 # ---- route ----------------------------------------------------------------------
@@ -181,44 +205,45 @@ def route_tensors(logits, experts, weights, slots, counts, prob_sums, loss, rows
     """taccl_route: experts int32, weights float32 and slots int32
     [tokens, k], counts int32 and prob_sums float32 [experts], loss float32
     [1] and rows int32 [1] from logits [tokens, experts]; mask uint8 [tokens]."""
-    (n, e), dtype = _matrix(logits, "logits")
-    p, stride = _rows(logits, "logits", (n, e), dtype)
+    (n, e), dtype, code, device = _matrix(logits, "logits")
+    p, stride = _rows(logits, "logits", (n, e), dtype, device)
     if experts.dim() != 2:
         raise ValueError("experts must be a matrix [tokens, k]")
     shape = (n, experts.shape[1])
-    m = None if mask is None else _flat(mask, "mask", (n,), torch.uint8)
-    w, w_bytes = _bytes(workspace, "workspace")
+    m = None if mask is None else _flat(mask, "mask", (n,), torch.uint8, device)
+    w, w_bytes = _bytes(workspace, "workspace", device)
     _call("taccl_route",
-          _Route(n, e, shape[1], _DTYPES[dtype], 1 if renorm else 0, coef, capacity, p, stride, m,
-                 _flat(experts, "experts", shape, torch.int32),
-                 _flat(weights, "weights", shape, torch.float32),
-                 _flat(slots, "slots", shape, torch.int32),
-                 _flat(counts, "counts", (e,), torch.int32),
-                 _flat(prob_sums, "prob_sums", (e,), torch.float32),
-                 _flat(loss, "loss", (1,), torch.float32),
-                 _flat(rows, "rows", (1,), torch.int32), w, w_bytes), stream)
+          _Route(n, e, shape[1], code, 1 if renorm else 0, coef, capacity, p, stride, m,
+                 _flat(experts, "experts", shape, torch.int32, device),
+                 _flat(weights, "weights", shape, torch.float32, device),
+                 _flat(slots, "slots", shape, torch.int32, device),
+                 _flat(counts, "counts", (e,), torch.int32, device),
+                 _flat(prob_sums, "prob_sums", (e,), torch.float32, device),
+                 _flat(loss, "loss", (1,), torch.float32, device),
+                 _flat(rows, "rows", (1,), torch.int32, device), w, w_bytes), device, stream)
 
 
 def route_backward_tensors(logits, experts, counts, rows, dlogits, *, dweights=None, dloss=None,
                            mask=None, coef=0.01, renorm=True, stream=None):
     """taccl_route_backward: dlogits from dweights [tokens, k] and dloss [1]
     (float32; None: zero). counts and rows may be summed over ranks."""
-    (n, e), dtype = _matrix(logits, "logits")
-    p, stride = _rows(logits, "logits", (n, e), dtype)
-    o, o_stride = _rows(dlogits, "dlogits", (n, e), dtype)
+    (n, e), dtype, code, device = _matrix(logits, "logits")
+    p, stride = _rows(logits, "logits", (n, e), dtype, device)
+    o, o_stride = _rows(dlogits, "dlogits", (n, e), dtype, device)
     if experts.dim() != 2:
         raise ValueError("experts must be a matrix [tokens, k]")
     shape = (n, experts.shape[1])
     _call("taccl_route_backward",
-          _RouteBackward(n, e, shape[1], _DTYPES[dtype], 1 if renorm else 0, coef, p, stride,
-                         None if mask is None else _flat(mask, "mask", (n,), torch.uint8),
-                         _flat(experts, "experts", shape, torch.int32),
-                         _flat(counts, "counts", (e,), torch.int32),
-                         _flat(rows, "rows", (1,), torch.int32),
+          _RouteBackward(n, e, shape[1], code, 1 if renorm else 0, coef, p, stride,
+                         None if mask is None else _flat(mask, "mask", (n,), torch.uint8, device),
+                         _flat(experts, "experts", shape, torch.int32, device),
+                         _flat(counts, "counts", (e,), torch.int32, device),
+                         _flat(rows, "rows", (1,), torch.int32, device),
                          None if dweights is None else
-                         _flat(dweights, "dweights", shape, torch.float32),
-                         None if dloss is None else _flat(dloss, "dloss", (1,), torch.float32),
-                         o, o_stride), stream)
+                         _flat(dweights, "dweights", shape, torch.float32, device),
+                         None if dloss is None else
+                         _flat(dloss, "dloss", (1,), torch.float32, device),
+                         o, o_stride), device, stream)
 
 
 # ---- dispatch and combine ---------------------------------------------------------
@@ -234,70 +259,75 @@ def chunk_bytes(num_experts, capacity, row_bytes, ranks, chunks_per_pair=1):
     return total // (ranks * chunks_per_pair)
 
 
-def _choices(experts, slots):
+def _choices(experts, slots, device):
     """(tokens, k, pointers) of the choices."""
     if experts.dim() != 2:
         raise ValueError("experts must be a matrix [tokens, k]")
     shape = experts.shape
-    return shape, _flat(experts, "experts", shape, torch.int32), \
-        _flat(slots, "slots", shape, torch.int32)
+    return shape, _flat(experts, "experts", shape, torch.int32, device), \
+        _flat(slots, "slots", shape, torch.int32, device)
 
 
 def _buffer(t, name):
-    if t.dim() != 3 or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous CUDA tensor [experts, capacity, dim]")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, not on the current device")
-    return t.shape
+    """(shape, device) of a buffer."""
+    if t.dim() != 3 or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{name} must be a contiguous CUDA tensor [experts, capacity, dim], got "
+                         f"{list(t.shape)} with strides {t.stride()} on {t.device}")
+    return t.shape, _on_device(t, name)
 
 
 def dispatch_tensors(x, experts, slots, counts, out, *, scale=None, out_scale=None, stream=None):
     """taccl_dispatch: out[experts[t, j], slots[t, j]] = x[t], zero from
     counts on; scale [tokens, n] float32 goes to out_scale [experts, capacity,
     n] alike. x of any type of 1, 2 or 4 bytes."""
-    e, c, d = _buffer(out, "out")
-    (n, k), pe, ps = _choices(experts, slots)
-    p, stride = _rows(x, "x", (n, d), out.dtype)
+    (e, c, d), device = _buffer(out, "out")
+    (n, k), pe, ps = _choices(experts, slots, device)
+    p, stride = _rows(x, "x", (n, d), out.dtype, device)
     s = o = None
     s_cols = s_stride = 0
     if scale is not None:
         if out_scale is None or scale.dim() != 2:
             raise ValueError("scale must be a matrix and come with out_scale")
         s_cols = scale.shape[1]
-        s, s_stride = _rows(scale, "scale", (n, s_cols), torch.float32)
-        o = _flat(out_scale, "out_scale", (e, c, s_cols), torch.float32)
+        s, s_stride = _rows(scale, "scale", (n, s_cols), torch.float32, device)
+        o = _flat(out_scale, "out_scale", (e, c, s_cols), torch.float32, device)
     _call("taccl_dispatch",
           _Dispatch(n, c, e, k, d, x.element_size(), s_cols, p, stride, s, s_stride, pe, ps,
-                    _flat(counts, "counts", (e,), torch.int32), out.data_ptr(), o), stream)
+                    _flat(counts, "counts", (e,), torch.int32, device), out.data_ptr(), o),
+          device, stream)
 
 
 def combine_tensors(buffer, experts, slots, out, *, weights=None, stream=None):
     """taccl_combine: out[t] = sum over j of weights[t, j] *
     buffer[experts[t, j], slots[t, j]] (weights None: 1)."""
-    e, c, d = _buffer(buffer, "buffer")
-    (n, k), pe, ps = _choices(experts, slots)
-    _, dtype = _matrix(out, "out")
-    o, o_stride = _rows(out, "out", (n, d), dtype)
-    w = None if weights is None else _flat(weights, "weights", (n, k), torch.float32)
+    shape, device = _buffer(buffer, "buffer")
+    e, c, d = shape
+    (n, k), pe, ps = _choices(experts, slots, device)
+    dtype = buffer.dtype
+    code = _code(dtype, "buffer")
+    o, o_stride = _rows(out, "out", (n, d), dtype, device)
+    w = None if weights is None else _flat(weights, "weights", (n, k), torch.float32, device)
     _call("taccl_combine",
-          _Combine(n, c, e, k, d, _DTYPES[dtype], _flat(buffer, "buffer", (e, c, d), dtype), pe, ps,
-                   w, o, o_stride), stream)
+          _Combine(n, c, e, k, d, code, buffer.data_ptr(), pe, ps, w, o, o_stride),
+          device, stream)
 
 
 def combine_backward_tensors(dout, buffer, experts, slots, counts, weights, dbuffer, dweights, *,
                              stream=None):
     """taccl_combine_backward: dbuffer (zero from counts on) and dweights."""
-    e, c, d = _buffer(buffer, "buffer")
-    (n, k), pe, ps = _choices(experts, slots)
-    _, dtype = _matrix(dout, "dout")
-    g, g_stride = _rows(dout, "dout", (n, d), dtype)
+    shape, device = _buffer(buffer, "buffer")
+    e, c, d = shape
+    (n, k), pe, ps = _choices(experts, slots, device)
+    dtype = buffer.dtype
+    code = _code(dtype, "buffer")
+    g, g_stride = _rows(dout, "dout", (n, d), dtype, device)
     _call("taccl_combine_backward",
-          _CombineBackward(n, c, e, k, d, _DTYPES[dtype], g, g_stride,
-                           _flat(buffer, "buffer", (e, c, d), dtype), pe, ps,
-                           _flat(counts, "counts", (e,), torch.int32),
-                           _flat(weights, "weights", (n, k), torch.float32),
-                           _flat(dbuffer, "dbuffer", (e, c, d), dtype),
-                           _flat(dweights, "dweights", (n, k), torch.float32)), stream)
+          _CombineBackward(n, c, e, k, d, code, g, g_stride, buffer.data_ptr(), pe, ps,
+                           _flat(counts, "counts", (e,), torch.int32, device),
+                           _flat(weights, "weights", (n, k), torch.float32, device),
+                           _flat(dbuffer, "dbuffer", shape, dtype, device),
+                           _flat(dweights, "dweights", (n, k), torch.float32, device)),
+          device, stream)
 
 
 # ---- differentiable forms ---------------------------------------------------------
