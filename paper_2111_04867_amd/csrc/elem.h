@@ -98,10 +98,16 @@ __device__ __forceinline__ void as_stored(V &v) {
   asm volatile("" : "+v"(v));
 }
 
+// Moves within a row of 16 lanes, every lane of it active: with the bound
+// control set there is no old value to keep, and the move becomes an operand
+// of what uses it.
+template <int Ctrl>
+__device__ __forceinline__ int dppi(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, Ctrl, 0xf, 0xf, true);
+}
 template <int Ctrl>
 __device__ __forceinline__ float dppf(float v) {
-  return __builtin_bit_cast(
-      float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), Ctrl, 0xf, 0xf, true));
+  return __builtin_bit_cast(float, dppi<Ctrl>(__builtin_bit_cast(int, v)));
 }
 constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
 constexpr int kRor8 = 0x128, kRor4 = 0x124, kRor2 = 0x122, kRor1 = 0x121;
@@ -132,10 +138,10 @@ __device__ __forceinline__ float lanes_max(float v) {
 }
 template <int L>
 __device__ __forceinline__ uint32_t lanes_min(uint32_t v) {
-  v = min(v, dpp<kRor8>(v));
-  v = min(v, dpp<kRor4>(v));
-  v = min(v, dpp<kRor2>(v));
-  v = min(v, dpp<kRor1>(v));
+  v = min(v, (uint32_t)dppi<kRor8>((int)v));
+  v = min(v, (uint32_t)dppi<kRor4>((int)v));
+  v = min(v, (uint32_t)dppi<kRor2>((int)v));
+  v = min(v, (uint32_t)dppi<kRor1>((int)v));
   if (L == 64) {
     v = min(v, (uint32_t)__shfl_xor((int)v, 16));
     v = min(v, (uint32_t)__shfl_xor((int)v, 32));

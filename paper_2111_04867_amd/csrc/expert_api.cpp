@@ -159,7 +159,7 @@ taccl_status_t taccl_norm_backward(const taccl_norm_backward_t *a, taccl_stream_
 }
 
 int64_t taccl_route_workspace(int32_t num_experts) {
-  const int64_t wide = ((int64_t)num_experts + 7) / 8 * 8;  // 6 bytes each, and a count
+  const int64_t wide = ((int64_t)num_experts + 7) / 8 * 8;  // rows of 6 bytes each, and a count
   return num_experts < 1 ? 0 : kRouteMaxBlocks * (8 * wide + 4);
 }
 

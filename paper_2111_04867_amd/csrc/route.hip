@@ -7,8 +7,17 @@
 //   renormalised (w = softmax over the chosen logits):
 //   dl_{e_j} += w_j (dw_j - sum_i w_i dw_i)
 //
-// A group of kL lanes holds one token's logits, kEpl experts per lane. The sums over tokens go through per-block partial results and a
-// second launch, never through floating atomics, so their order is fixed.
+// A group of kL lanes holds one token's logits, kEpl experts per lane. The sums
+// over tokens go through per-block partial results and a second launch, never
+// through floating atomics, so their order is fixed; a small batch takes one
+// block and one launch.
+//
+// What bounds it: 32768 tokens, 256 experts, 8 choices, f32 (33.5 MB, 7 us of
+// memory) take 17 us in the first launch, half of them vector instructions
+// (1150 per wavefront, that is for eight tokens), and 8 us in the second, which
+// is mostly launch and round trips to memory. 64 experts, 4 choices: 9 and 5.5
+// us. Taking the k maxima one after the other was 23 us where the threshold
+// below takes 17. The gradient (67 MB, 13 us of memory) takes 22 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -22,6 +31,10 @@ namespace {
 
 constexpr int kRouteThreads = 1024;
 constexpr int kBackThreads = 256;
+// up to kSmallTile tokens a block of 256 threads, up to kOneBlock one of 1024
+// (two launches: 11.6 instead of 9 us), up to kSmallBlocks blocks of 256 again,
+// so that the tokens are spread over the CUs (6000 tokens, 64 experts: 11.9 us,
+// 13.1 with 1024)
 constexpr int kSmallTile = 16, kOneBlock = 128, kSmallBlocks = 8192;
 
 // Per-block results: the experts' counts and probability sums in rows padded
@@ -49,33 +62,39 @@ struct TokenRow {
     return lane * kN + i / kN * (kL * kN) + i % kN;
   }
 
-  float v[kEpl];  // minus infinity past the experts and in rows not taken
-  __device__ __forceinline__ void load(const T *row, int lane, int E, bool take) {
-    if (take && E == kL * kEpl) {
+  // the logits as they are stored: minus infinity past the experts and in rows
+  // not taken
+  struct Raw {
+    W w[kSlots];
+    __device__ __forceinline__ void load(const T *row, int lane, int E, bool take) {
+#pragma unroll
+      for (int s = 0; s < kSlots; s++)
+#pragma unroll
+        for (int x = 0; x < kN; x++) w[s][x] = (T)-__builtin_inff();
+      if (!take) return;
+      if (E == kL * kEpl) {
+#pragma unroll
+        for (int s = 0; s < kSlots; s++) w[s] = *(const U *)(row + index(lane, s * kN));
+        return;
+      }
 #pragma unroll
       for (int s = 0; s < kSlots; s++) {
-        const W w = *(const U *)(row + index(lane, s * kN));
+        const int e = index(lane, s * kN);
+        if (e + kN <= E) {
+          w[s] = *(const U *)(row + e);
+        } else {
 #pragma unroll
-        for (int x = 0; x < kN; x++) v[s * kN + x] = (float)w[x];
-      }
-      return;
-    }
-#pragma unroll
-    for (int i = 0; i < kEpl; i++) v[i] = -__builtin_inff();
-    if (!take) return;
-#pragma unroll
-    for (int s = 0; s < kSlots; s++) {
-      const int e = index(lane, s * kN);
-      if (e + kN <= E) {
-        const W w = *(const U *)(row + e);
-#pragma unroll
-        for (int x = 0; x < kN; x++) v[s * kN + x] = (float)w[x];
-      } else {
-#pragma unroll
-        for (int x = 0; x < kN; x++)
-          if (e + x < E) v[s * kN + x] = (float)row[e + x];
+          for (int x = 0; x < kN; x++)
+            if (e + x < E) w[s][x] = row[e + x];
+        }
       }
     }
+  };
+
+  float v[kEpl];
+  __device__ __forceinline__ void take(const Raw &r) {
+#pragma unroll
+    for (int i = 0; i < kEpl; i++) v[i] = (float)r.w[i / kN][i % kN];
   }
 
   // Softmax: the lane's maximum and the exponent's offset (0 in a row of minus
@@ -128,20 +147,20 @@ __device__ __forceinline__ int row_rank(bool there, float logit, int expert, uin
   }
   if (!there) key = kNone;
   uint32_t rank = 0;
-#define BEATEN(R) rank += (int)dpp<0x120 + R>((uint32_t)key) > key ? 1u : 0u;
+#define BEATEN(R) rank += dppi<0x120 + R>(key) > key ? 1u : 0u;
   IN_ROW(BEATEN)
 #undef BEATEN
   if (sizeof(T) == 2) return (int)rank;
   uint32_t taken = there ? 1u << rank : 0u;
-  taken |= dpp<kRor8>(taken);
-  taken |= dpp<kRor4>(taken);
-  taken |= dpp<kRor2>(taken);
-  taken |= dpp<kRor1>(taken);
+  taken |= (uint32_t)dppi<kRor8>((int)taken);
+  taken |= (uint32_t)dppi<kRor4>((int)taken);
+  taken |= (uint32_t)dppi<kRor2>((int)taken);
+  taken |= (uint32_t)dppi<kRor1>((int)taken);
   if (!__any(taken != (1u << n) - 1)) return (int)rank;
 #define EQUAL(R)                                        \
   {                                                     \
-    const int k = (int)dpp<0x120 + R>((uint32_t)key);   \
-    const int x = (int)dpp<0x120 + R>((uint32_t)expert); \
+    const int k = dppi<0x120 + R>(key);                 \
+    const int x = dppi<0x120 + R>(expert);              \
     rank += k == key && x < expert ? 1u : 0u;           \
   }
   IN_ROW(EQUAL)
@@ -149,23 +168,23 @@ __device__ __forceinline__ int row_rank(bool there, float logit, int expert, uin
   return (int)rank;
 }
 
-// The row's values in descending order (bitonic merges over mirrored halves)
-__device__ __forceinline__ float row_sorted(float v, int lane) {
-  auto step = [&](float o, int bit) {
-    const float hi = fmaxf(v, o), lo = fminf(v, o);
+// The row's keys in descending order (bitonic merges over mirrored halves)
+__device__ __forceinline__ int row_sorted(int v, int lane) {
+  auto step = [&](int o, int bit) {
+    const int hi = max(v, o), lo = min(v, o);
     v = lane & bit ? lo : hi;
   };
   constexpr int kMirror4 = 0x1B;  // quad_perm [3, 2, 1, 0]
-  step(dppf<kXor1>(v), 1);
-  step(dppf<kMirror4>(v), 2);
-  step(dppf<kXor1>(v), 1);
-  step(dppf<kHalfMirror>(v), 4);
-  step(dppf<kXor2>(v), 2);
-  step(dppf<kXor1>(v), 1);
-  step(dppf<kMirror>(v), 8);
-  step(dppf<kMirror4>(dppf<kHalfMirror>(v)), 4);
-  step(dppf<kXor2>(v), 2);
-  step(dppf<kXor1>(v), 1);
+  step(dppi<kXor1>(v), 1);
+  step(dppi<kMirror4>(v), 2);
+  step(dppi<kXor1>(v), 1);
+  step(dppi<kHalfMirror>(v), 4);
+  step(dppi<kXor2>(v), 2);
+  step(dppi<kXor1>(v), 1);
+  step(dppi<kMirror>(v), 8);
+  step(dppi<kMirror4>(dppi<kHalfMirror>(v)), 4);
+  step(dppi<kXor2>(v), 2);
+  step(dppi<kXor1>(v), 1);
   return v;
 }
 
@@ -179,6 +198,7 @@ struct Choice {
 template <class T, int kL, int kEpl>
 __device__ __forceinline__ Choice choose_each(TokenRow<T, kL, kEpl> &x, int k, int lane) {
   Choice c{lane, -1, 0.0f};
+  asm volatile("" : "+v"(lane));  // nothing of this is worked out ahead, where it is seldom used
   for (int j = 0; j < k; j++) {
     float m = -__builtin_inff();
 #pragma unroll
@@ -204,20 +224,26 @@ __device__ __forceinline__ Choice choose_each(TokenRow<T, kL, kEpl> &x, int k, i
 // largest logit from below, so the choices are among the logits that reach it.
 // Where at most 16 do (for k = 8 about 10 of 256 random ones, 0.7% of the rows
 // have more), lanes 0 to 15 of the group take one each, and their ranks are
-// the choice. list_ranked() finds the candidates and has their
-// logits loaded again (a lane's element is no register index), to be used
-// behind the exponentials by rank_listed(). False: some row of the wavefront
-// has more.
+// the choice. list_ranked() finds the candidates and reads their logits from
+// the group's row in LDS (a lane's element is no register index; read from
+// memory, they would have to wait for the next tile's logits, which are on
+// their way), to be used behind the exponentials by rank_listed(). False: some
+// row of the wavefront has more.
 template <class T, int kL, int kEpl>
 __device__ __forceinline__ bool list_ranked(const TokenRow<T, kL, kEpl> &x, int k, int lane,
-                                            const T *row, uint16_t *list, Choice &c,
+                                            float *stage, uint16_t *list, Choice &c,
                                             uint32_t &n) {
   typedef TokenRow<T, kL, kEpl> Row;
   // at least the lowest number: minus infinities are never chosen
   float bound = -__FLT_MAX__;
   if (kL == 16) {
-    const float sorted = fmaxf(row_sorted(x.top, lane), bound);  // by every lane of the row
-    bound = lanes_max<16>(lane == k - 1 ? sorted : bound);
+    const int sorted = row_sorted(order_key(x.top), lane);  // by every lane of the row
+    int b = lane == k - 1 ? sorted : kNone;
+    b = max(b, dppi<kRor8>(b));
+    b = max(b, dppi<kRor4>(b));
+    b = max(b, dppi<kRor2>(b));
+    b = max(b, dppi<kRor1>(b));
+    bound = fmaxf(bound, __builtin_bit_cast(float, b ^ ((b >> 31) & 0x7FFFFFFF)));
   } else {
     float m = x.top, most = m;
     for (int j = 0; j < k; j++) {  // the lanes' maxima, one lane after the other
@@ -230,15 +256,18 @@ __device__ __forceinline__ bool list_ranked(const TokenRow<T, kL, kEpl> &x, int 
   uint32_t hit = 0;
 #pragma unroll
   for (int i = 0; i < kEpl; i++) hit |= x.v[i] >= bound ? 1u << i : 0u;
+#pragma unroll
+  for (int i = 0; i < kEpl; i++) stage[Row::index(lane, i)] = x.v[i];
   const uint32_t mine = __popc(hit);
   const uint32_t upto = kL == 16 ? row_scan_add(mine) : wave_scan_add(mine);
   const uint32_t all = kL == 16 ? dpp<0x15F>(upto)  // the row's last lane
                                 : (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
   if (__any(all > 16)) return false;
   uint32_t at = upto - mine;
+  const uint32_t first = (uint32_t)lane * Row::kN;  // Row::index(lane, 0)
   do {  // a lane without a further one writes past the list
-    const int i = __ffs(hit) - 1;
-    list[hit ? at : 16] = (uint16_t)Row::index(lane, i);
+    const uint32_t i = (uint32_t)__builtin_ctz(hit | 1u << 31);
+    list[hit ? at : 16] = (uint16_t)(first + i + i / Row::kN * (kL * Row::kN - Row::kN));
     hit &= hit - 1;
     at++;
   } while (__any(hit));
@@ -248,7 +277,7 @@ __device__ __forceinline__ bool list_ranked(const TokenRow<T, kL, kEpl> &x, int 
   c = Choice{lane, -1, 0.0f};
   if ((uint32_t)lane < all) {
     c.expert = list[lane];
-    c.logit = (float)row[c.expert];
+    c.logit = stage[c.expert];
   }
   __builtin_amdgcn_wave_barrier();
   asm volatile("" ::: "memory");
@@ -307,7 +336,9 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
   constexpr int kWaves = kRouteThreads / 64, kCols = kL * kEpl;
   __shared__ uint64_t bits[kCols + 1][kWords];
   __shared__ uint32_t cnt[kCols + 1];
-  __shared__ float sums[kWaves][kCols];
+  // a tile's logits, and behind the last tile the wavefronts' sums
+  __shared__ __align__(16) float stage[kRanked ? kRouteThreads / kL : kWaves][kCols];
+  float (*sums)[kCols] = stage;
   __shared__ float red[kWaves];
   __shared__ uint16_t list[kRanked ? kRouteThreads / kL : 1][16 + 1];
   __shared__ int16_t picked[kStep * kMaxChoices];  // expert of every choice of the step
@@ -323,6 +354,14 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
   for (int i = 0; i < kEpl; i++) acc[i] = 0;
   const int64_t begin = (int64_t)blockIdx.x * part.per_block;
   const int64_t end = min(begin + part.per_block, a.tokens);
+  // a tile's logits are on their way while the one before is worked on
+  typedef TokenRow<T, kL, kEpl> Row;
+  typename Row::Raw next;
+  auto fetch = [&](int64_t t) {
+    next.load((const T *)a.logits + t * a.logits_stride, lane, E,
+              t < end && (!a.mask || a.mask[t]));
+  };
+  fetch(begin + group);
   __syncthreads();
   for (int64_t first = begin; first < end; first += kStep) {
     const int n = (int)min((int64_t)kStep, end - first);  // tokens of the step
@@ -330,14 +369,16 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
       const int at = tile + group;
       const int64_t t = first + at;
       const bool inside = at < n;
-      const bool take = inside && (!a.mask || a.mask[t]);
-      const T *row = (const T *)a.logits + t * a.logits_stride;
-      TokenRow<T, kL, kEpl> x;
-      x.load(row, lane, E, take);
+      Row x;
+      x.take(next);
+      // the wait for this tile's loads comes before the next tile's are issued
+#pragma unroll
+      for (int i = 0; i < kEpl; i++) asm volatile("" : "+v"(x.v[i]));
+      fetch(t + groups);
       x.maxima();
       Choice c;
       uint32_t n_listed = 0;
-      const bool listed = kRanked && list_ranked(x, k, lane, row, list[group], c, n_listed);
+      const bool listed = kRanked && list_ranked(x, k, lane, stage[group], list[group], c, n_listed);
       x.exponentials();
 #pragma unroll
       for (int i = 0; i < kEpl; i++) acc[i] += x.p[i] * x.inv;
@@ -365,13 +406,9 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
       const int e = picked[i], at = i / k;
       int slot = -1;
       if (e >= 0) {
-        uint32_t place = cnt[e];
-#pragma unroll
-        for (int w = 0; w < kWords; w++) {
-          const int past = at - 64 * w;  // bits of this word below the token's
-          const uint64_t below = past >= 64 ? ~0ull : past > 0 ? (1ull << past) - 1 : 0ull;
-          place += (uint32_t)__popcll(bits[e][w] & below);
-        }
+        const int word = at >> 6;
+        uint32_t place = cnt[e] + (uint32_t)__popcll(bits[e][word] & ((1ull << (at & 63)) - 1));
+        for (int w = 0; w < word; w++) place += (uint32_t)__popcll(bits[e][w]);
         slot = part.blocks > 1 || !a.capacity || place < a.capacity ? (int)place : -1;
       }
       a.slots[first * k + i] = slot;
@@ -388,7 +425,6 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
   }
   // the block's probability sums: rows of a wavefront, then wavefronts
   float *mine = sums[threadIdx.x >> 6];
-  typedef TokenRow<T, kL, kEpl> Row;
   if (kL == 64) {
 #pragma unroll
     for (int i = 0; i < kEpl; i++) mine[Row::index(lane, i)] = acc[i];
@@ -467,7 +503,9 @@ struct ColumnSums {
 // Second launch: block b adds the counts of the blocks before b to the
 // places of b's choices; the block behind them finishes the totals. Each
 // loads what it needs at once: a round trip to memory is the larger part of
-// its time.
+// its time. The last block takes longest, 3 us for what one CU reads of 256
+// blocks and experts; dealt out over eight blocks, the fences that their totals
+// need took 6 us more than that saved.
 __global__ __launch_bounds__(kRouteThreads) void route_places_kernel(taccl_route_t a,
                                                                      RoutePartial part) {
   __shared__ __align__(16) uint32_t lds[8 * kRouteThreads];
@@ -543,8 +581,10 @@ __global__ __launch_bounds__(kBackThreads) void route_backward_kernel(taccl_rout
       expert = a.experts[t * k + lane];
       dw = a.dweights[t * k + lane];
     }
+    typename Row::Raw raw;
+    raw.load(row, lane, E, take);
     Row x;
-    x.load(row, lane, E, take);
+    x.take(raw);
     if ((uint32_t)expert < (uint32_t)E) weight = (float)row[expert];
     else expert = -1;
     x.maxima();
