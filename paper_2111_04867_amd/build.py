@@ -1,4 +1,5 @@
-"""Build the evaluator library (HIP for gfx950) into paper_2111_04867_amd/libtaccl.so."""
+"""Build the library (HIP for gfx950) into paper_2111_04867_amd/libtaccl.so and
+the expert-layer binding beside it."""
 import glob
 import os
 import subprocess
@@ -86,5 +87,30 @@ def build_library(verbose=False, jobs=8, only_changed=False, sanitize=False):
     return out
 
 
+def build_experts_binding(verbose=False):
+    """Compile pyext/experts.cpp (host code against torch's headers) into the
+    extension module _experts."""
+    import sysconfig
+
+    import torch
+
+    base = os.path.dirname(torch.__file__)
+    inc = [sysconfig.get_paths()["include"], os.path.join(base, "include"),
+           os.path.join(base, "include", "torch", "csrc", "api", "include"),
+           os.path.join(ROOT, "include")]
+    out = os.path.join(PKG, "_experts.so")
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    cmd += [f"-isystem{d}" if d.startswith(base) else f"-I{d}" for d in inc]
+    cmd += [os.path.join(PKG, "pyext", "experts.cpp"), "-o", out + ".tmp",
+            "-L" + os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.run(cmd, check=True)
+    os.replace(out + ".tmp", out)
+    return out
+
+
 if __name__ == "__main__":
     print(build_library(verbose=True))
+    print(build_experts_binding(verbose=True))

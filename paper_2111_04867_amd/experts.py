@@ -20,71 +20,25 @@ import torch
 
 from . import binding
 
-_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-_P, _I32, _I64, _F32 = ct.c_void_p, ct.c_int32, ct.c_int64, ct.c_float
+try:
+    from . import _experts as _calls
+except ImportError as e:
+    raise ImportError("paper_2111_04867_amd/_experts.so is missing or does not load: build it with "
+                      f"__graft_entry__.build() ({e})") from e
 
 
-def _struct(name, fields):
-    return type(name, (ct.Structure,), {"_fields_": fields})
+def _address(name):
+    return ct.cast(getattr(binding.lib(), "taccl_" + name), ct.c_void_p).value
 
 
-# argument structs of include/taccl.h, in their order
-_Norm = _struct("_Norm", [
-    ("rows", _I64), ("cols", _I32), ("dtype", _I32), ("eps", _F32), ("group", _I32), ("x", _P),
-    ("residual", _P), ("x_stride", _I64), ("residual_stride", _I64), ("weight", _P), ("out", _P),
-    ("total", _P), ("out_stride", _I64), ("total_stride", _I64), ("q", _P), ("scale", _P),
-    ("q_stride", _I64), ("scale_stride", _I64)])
-_NormBackward = _struct("_NormBackward", [
-    ("rows", _I64), ("cols", _I32), ("dtype", _I32), ("eps", _F32), ("dout", _P), ("h", _P),
-    ("dtotal", _P), ("dout_stride", _I64), ("h_stride", _I64), ("dtotal_stride", _I64),
-    ("weight", _P), ("dx", _P), ("dx_stride", _I64), ("dweight", _P), ("workspace", _P),
-    ("workspace_bytes", _I64)])
-_Route = _struct("_Route", [
-    ("tokens", _I64), ("num_experts", _I32), ("k", _I32), ("dtype", _I32), ("renorm", _I32),
-    ("coef", _F32), ("capacity", _I64), ("logits", _P), ("logits_stride", _I64), ("mask", _P),
-    ("experts", _P), ("weights", _P), ("slots", _P), ("counts", _P), ("prob_sums", _P),
-    ("loss", _P), ("rows", _P), ("workspace", _P), ("workspace_bytes", _I64)])
-_RouteBackward = _struct("_RouteBackward", [
-    ("tokens", _I64), ("num_experts", _I32), ("k", _I32), ("dtype", _I32), ("renorm", _I32),
-    ("coef", _F32), ("logits", _P), ("logits_stride", _I64), ("mask", _P), ("experts", _P),
-    ("counts", _P), ("rows", _P), ("dweights", _P), ("dloss", _P), ("dlogits", _P),
-    ("dlogits_stride", _I64)])
-_Dispatch = _struct("_Dispatch", [
-    ("tokens", _I64), ("capacity", _I64), ("num_experts", _I32), ("k", _I32), ("cols", _I32),
-    ("element_bytes", _I32), ("scale_cols", _I32), ("x", _P), ("x_stride", _I64), ("scale", _P),
-    ("scale_stride", _I64), ("experts", _P), ("slots", _P), ("counts", _P), ("out", _P),
-    ("out_scale", _P)])
-_Combine = _struct("_Combine", [
-    ("tokens", _I64), ("capacity", _I64), ("num_experts", _I32), ("k", _I32), ("cols", _I32),
-    ("dtype", _I32), ("buffer", _P), ("experts", _P), ("slots", _P), ("weights", _P), ("out", _P),
-    ("out_stride", _I64)])
-_CombineBackward = _struct("_CombineBackward", [
-    ("tokens", _I64), ("capacity", _I64), ("num_experts", _I32), ("k", _I32), ("cols", _I32),
-    ("dtype", _I32), ("dout", _P), ("dout_stride", _I64), ("buffer", _P), ("experts", _P),
-    ("slots", _P), ("counts", _P), ("weights", _P), ("dbuffer", _P), ("dweights", _P)])
-
-_calls = {}
-
-
-def _bind(name):
-    fn = getattr(binding.lib(), name)
-    fn.argtypes, fn.restype = [_P, _P], ct.c_int
-    _calls[name] = fn
-    return fn
-
-
-def _call(name, args, device, stream):
-    """The library's call on `stream`, or on the current one of `device`."""
-    fn = _calls.get(name) or _bind(name)
-    status = fn(ct.addressof(args), torch._C._cuda_getCurrentRawStream(device)
-                if stream is None else stream.cuda_stream)
-    if status:
-        binding._check(status)
+_calls.bind(torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
+            *(_address(n) for n in ("norm", "norm_backward", "route", "route_backward", "dispatch",
+                                    "combine", "combine_backward")))
 
 
 def _size(name, arg):
     fn = getattr(binding.lib(), name)
-    fn.argtypes, fn.restype = [_I32], _I64
+    fn.argtypes, fn.restype = [ct.c_int32], ct.c_int64
     return fn(arg)
 
 
@@ -98,156 +52,6 @@ def route_workspace(num_experts):
     return _size("taccl_route_workspace", int(num_experts))
 
 
-def _wrong(t, name, what, shape, dtype):
-    return ValueError(f"{name} must be a {what} {list(shape)} of {dtype}, got {list(t.shape)} of "
-                      f"{t.dtype} with strides {t.stride()} on {t.device}")
-
-
-def _rows(t, name, shape, dtype, device):
-    """(pointer, row stride) of a matrix on `device` with a contiguous last axis."""
-    if t.dtype is dtype and t.get_device() == device and t.shape == shape:
-        stride = t.stride()
-        if stride[1] == 1 or shape[1] <= 1:
-            return t.data_ptr(), stride[0]
-    raise _wrong(t, name, "CUDA tensor with contiguous rows", shape, dtype)
-
-
-def _flat(t, name, shape, dtype, device):
-    """Pointer of a contiguous tensor on `device`."""
-    if t.dtype is dtype and t.get_device() == device and t.shape == shape and t.is_contiguous():
-        return t.data_ptr()
-    raise _wrong(t, name, "contiguous CUDA tensor", shape, dtype)
-
-
-def _on_device(t, name):
-    """Index of the tensor's device, which has to be the current one."""
-    device = t.get_device()
-    if device < 0 or device != torch._C._cuda_getDevice():
-        raise ValueError(f"{name} must be a CUDA tensor on the current device, is on {t.device}")
-    return device
-
-
-def _matrix(t, name):
-    """(shape, type, its code, device) of the tensor that a call's others go by."""
-    dtype = t.dtype
-    code = _DTYPES.get(dtype)
-    if code is None or t.dim() != 2:
-        raise ValueError(f"{name} must be a matrix of {', '.join(str(d) for d in _DTYPES)}, got "
-                         f"{list(t.shape)} of {dtype}")
-    return t.shape, dtype, code, _on_device(t, name)
-
-
-def _code(dtype, name):
-    code = _DTYPES.get(dtype)
-    if code is None:
-        raise ValueError(f"{name} is of {dtype}, must be one of {', '.join(map(str, _DTYPES))}")
-    return code
-
-
-def _bytes(t, name, device):
-    if t.get_device() != device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous CUDA tensor on the current device")
-    return t.data_ptr(), t.numel() * t.element_size()
-
-
-# ---- norm -----------------------------------------------------------------------
-
-def norm_tensors(x, weight, out=None, *, eps=1e-6, residual=None, total=None, q=None, scale=None,
-                 group=128, stream=None):
-    """taccl_norm: h = x + residual; out = weight * h / sqrt(mean(h^2) + eps);
-    total = h; q (float8_e4m3fn) = out / scale, scale [rows, ceil(cols /
-    group)] in 32 bits (group 0: one column). Outputs that are None are left
-    out."""
-    shape, dtype, code, device = _matrix(x, "x")
-    n, d = shape
-    p, stride = _rows(x, "x", shape, dtype, device)
-    r = o = h = f = s = None
-    r_stride = o_stride = h_stride = f_stride = s_stride = 0
-    if residual is not None:
-        r, r_stride = _rows(residual, "residual", shape, dtype, device)
-    if out is not None:
-        o, o_stride = _rows(out, "out", shape, dtype, device)
-    if total is not None:
-        h, h_stride = _rows(total, "total", shape, dtype, device)
-    if q is not None:
-        f, f_stride = _rows(q, "q", shape, torch.float8_e4m3fn, device)
-    if scale is not None:
-        s, s_stride = _rows(scale, "scale", (n, -(-d // group) if group else 1), torch.float32,
-                            device)
-    w = _flat(weight, "weight", (d,), dtype, device)
-    _call("taccl_norm", _Norm(n, d, code, eps, group, p, r, stride, r_stride, w, o, h, o_stride,
-                              h_stride, f, s, f_stride, s_stride), device, stream)
-
-
-def norm_backward_tensors(dout, h, weight, dx, dweight, workspace, *, eps=1e-6, dtotal=None,
-                          stream=None):
-    """taccl_norm_backward: dx (of x and of residual) and dweight (32 bits)
-    from dout, the stored total h and the gradient dtotal that reaches h
-    directly."""
-    shape, dtype, code, device = _matrix(h, "h")
-    n, d = shape
-    g, g_stride = _rows(dout, "dout", shape, dtype, device)
-    p, stride = _rows(h, "h", shape, dtype, device)
-    t, t_stride = (None, 0) if dtotal is None else _rows(dtotal, "dtotal", shape, dtype, device)
-    o, o_stride = _rows(dx, "dx", shape, dtype, device)
-    w, w_bytes = _bytes(workspace, "workspace", device)
-    _call("taccl_norm_backward",
-          _NormBackward(n, d, code, eps, g, p, t, g_stride, stride, t_stride,
-                        _flat(weight, "weight", (d,), dtype, device), o, o_stride,
-                        _flat(dweight, "dweight", (d,), torch.float32, device), w, w_bytes),
-          device, stream)
-
-
-# ---- route ----------------------------------------------------------------------
-
-def route_tensors(logits, experts, weights, slots, counts, prob_sums, loss, rows, workspace, *,
-                  mask=None, capacity=0, coef=0.01, renorm=True, stream=None):
-    """taccl_route: experts int32, weights float32 and slots int32
-    [tokens, k], counts int32 and prob_sums float32 [experts], loss float32
-    [1] and rows int32 [1] from logits [tokens, experts]; mask uint8 [tokens]."""
-    (n, e), dtype, code, device = _matrix(logits, "logits")
-    p, stride = _rows(logits, "logits", (n, e), dtype, device)
-    if experts.dim() != 2:
-        raise ValueError("experts must be a matrix [tokens, k]")
-    shape = (n, experts.shape[1])
-    m = None if mask is None else _flat(mask, "mask", (n,), torch.uint8, device)
-    w, w_bytes = _bytes(workspace, "workspace", device)
-    _call("taccl_route",
-          _Route(n, e, shape[1], code, 1 if renorm else 0, coef, capacity, p, stride, m,
-                 _flat(experts, "experts", shape, torch.int32, device),
-                 _flat(weights, "weights", shape, torch.float32, device),
-                 _flat(slots, "slots", shape, torch.int32, device),
-                 _flat(counts, "counts", (e,), torch.int32, device),
-                 _flat(prob_sums, "prob_sums", (e,), torch.float32, device),
-                 _flat(loss, "loss", (1,), torch.float32, device),
-                 _flat(rows, "rows", (1,), torch.int32, device), w, w_bytes), device, stream)
-
-
-def route_backward_tensors(logits, experts, counts, rows, dlogits, *, dweights=None, dloss=None,
-                           mask=None, coef=0.01, renorm=True, stream=None):
-    """taccl_route_backward: dlogits from dweights [tokens, k] and dloss [1]
-    (float32; None: zero). counts and rows may be summed over ranks."""
-    (n, e), dtype, code, device = _matrix(logits, "logits")
-    p, stride = _rows(logits, "logits", (n, e), dtype, device)
-    o, o_stride = _rows(dlogits, "dlogits", (n, e), dtype, device)
-    if experts.dim() != 2:
-        raise ValueError("experts must be a matrix [tokens, k]")
-    shape = (n, experts.shape[1])
-    _call("taccl_route_backward",
-          _RouteBackward(n, e, shape[1], code, 1 if renorm else 0, coef, p, stride,
-                         None if mask is None else _flat(mask, "mask", (n,), torch.uint8, device),
-                         _flat(experts, "experts", shape, torch.int32, device),
-                         _flat(counts, "counts", (e,), torch.int32, device),
-                         _flat(rows, "rows", (1,), torch.int32, device),
-                         None if dweights is None else
-                         _flat(dweights, "dweights", shape, torch.float32, device),
-                         None if dloss is None else
-                         _flat(dloss, "dloss", (1,), torch.float32, device),
-                         o, o_stride), device, stream)
-
-
-# ---- dispatch and combine ---------------------------------------------------------
-
 def chunk_bytes(num_experts, capacity, row_bytes, ranks, chunks_per_pair=1):
     """Bytes of an Alltoall chunk that carries one rank's share of a dispatch
     buffer: num_experts / ranks experts of `capacity` rows each, split over
@@ -259,75 +63,80 @@ def chunk_bytes(num_experts, capacity, row_bytes, ranks, chunks_per_pair=1):
     return total // (ranks * chunks_per_pair)
 
 
-def _choices(experts, slots, device):
-    """(tokens, k, pointers) of the choices."""
-    if experts.dim() != 2:
-        raise ValueError("experts must be a matrix [tokens, k]")
-    shape = experts.shape
-    return shape, _flat(experts, "experts", shape, torch.int32, device), \
-        _flat(slots, "slots", shape, torch.int32, device)
+# ---- on the caller's tensors --------------------------------------------------------
+# The tensors are checked (ValueError) and the library called (TacclError) in
+# pyext/experts.cpp. All have to be on the current device; matrices may have
+# rows further apart than their length.
+
+def norm_tensors(x, weight, out=None, *, eps=1e-6, residual=None, total=None, q=None, scale=None,
+                 group=128, stream=None):
+    """taccl_norm: h = x + residual; out = weight * h / sqrt(mean(h^2) + eps);
+    total = h; q (float8_e4m3fn) = out / scale, scale [rows, ceil(cols /
+    group)] in 32 bits (group 0: one column). Outputs that are None are left
+    out."""
+    st = _calls.norm(x, weight, out, eps, residual, total, q, scale, group,
+                     stream and stream.cuda_stream)
+    if st:
+        binding._check(st)
 
 
-def _buffer(t, name):
-    """(shape, device) of a buffer."""
-    if t.dim() != 3 or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{name} must be a contiguous CUDA tensor [experts, capacity, dim], got "
-                         f"{list(t.shape)} with strides {t.stride()} on {t.device}")
-    return t.shape, _on_device(t, name)
+def norm_backward_tensors(dout, h, weight, dx, dweight, workspace, *, eps=1e-6, dtotal=None,
+                          stream=None):
+    """taccl_norm_backward: dx (of x and of residual) and dweight (32 bits)
+    from dout, the stored total h and the gradient dtotal that reaches h
+    directly."""
+    st = _calls.norm_backward(dout, h, weight, dx, dweight, workspace, eps, dtotal,
+                              stream and stream.cuda_stream)
+    if st:
+        binding._check(st)
+
+
+def route_tensors(logits, experts, weights, slots, counts, prob_sums, loss, rows, workspace, *,
+                  mask=None, capacity=0, coef=0.01, renorm=True, stream=None):
+    """taccl_route: experts int32, weights float32 and slots int32
+    [tokens, k], counts int32 and prob_sums float32 [experts], loss float32
+    [1] and rows int32 [1] from logits [tokens, experts]; mask uint8 [tokens]."""
+    st = _calls.route(logits, experts, weights, slots, counts, prob_sums, loss, rows, workspace,
+                      mask, capacity, coef, renorm, stream and stream.cuda_stream)
+    if st:
+        binding._check(st)
+
+
+def route_backward_tensors(logits, experts, counts, rows, dlogits, *, dweights=None, dloss=None,
+                           mask=None, coef=0.01, renorm=True, stream=None):
+    """taccl_route_backward: dlogits from dweights [tokens, k] and dloss [1]
+    (float32; None: zero). counts and rows may be summed over ranks."""
+    st = _calls.route_backward(logits, experts, counts, rows, dlogits, dweights, dloss, mask, coef,
+                               renorm, stream and stream.cuda_stream)
+    if st:
+        binding._check(st)
 
 
 def dispatch_tensors(x, experts, slots, counts, out, *, scale=None, out_scale=None, stream=None):
     """taccl_dispatch: out[experts[t, j], slots[t, j]] = x[t], zero from
     counts on; scale [tokens, n] float32 goes to out_scale [experts, capacity,
     n] alike. x of any type of 1, 2 or 4 bytes."""
-    (e, c, d), device = _buffer(out, "out")
-    (n, k), pe, ps = _choices(experts, slots, device)
-    p, stride = _rows(x, "x", (n, d), out.dtype, device)
-    s = o = None
-    s_cols = s_stride = 0
-    if scale is not None:
-        if out_scale is None or scale.dim() != 2:
-            raise ValueError("scale must be a matrix and come with out_scale")
-        s_cols = scale.shape[1]
-        s, s_stride = _rows(scale, "scale", (n, s_cols), torch.float32, device)
-        o = _flat(out_scale, "out_scale", (e, c, s_cols), torch.float32, device)
-    _call("taccl_dispatch",
-          _Dispatch(n, c, e, k, d, x.element_size(), s_cols, p, stride, s, s_stride, pe, ps,
-                    _flat(counts, "counts", (e,), torch.int32, device), out.data_ptr(), o),
-          device, stream)
+    st = _calls.dispatch(x, experts, slots, counts, out, scale, out_scale,
+                         stream and stream.cuda_stream)
+    if st:
+        binding._check(st)
 
 
 def combine_tensors(buffer, experts, slots, out, *, weights=None, stream=None):
     """taccl_combine: out[t] = sum over j of weights[t, j] *
     buffer[experts[t, j], slots[t, j]] (weights None: 1)."""
-    shape, device = _buffer(buffer, "buffer")
-    e, c, d = shape
-    (n, k), pe, ps = _choices(experts, slots, device)
-    dtype = buffer.dtype
-    code = _code(dtype, "buffer")
-    o, o_stride = _rows(out, "out", (n, d), dtype, device)
-    w = None if weights is None else _flat(weights, "weights", (n, k), torch.float32, device)
-    _call("taccl_combine",
-          _Combine(n, c, e, k, d, code, buffer.data_ptr(), pe, ps, w, o, o_stride),
-          device, stream)
+    st = _calls.combine(buffer, experts, slots, out, weights, stream and stream.cuda_stream)
+    if st:
+        binding._check(st)
 
 
 def combine_backward_tensors(dout, buffer, experts, slots, counts, weights, dbuffer, dweights, *,
                              stream=None):
     """taccl_combine_backward: dbuffer (zero from counts on) and dweights."""
-    shape, device = _buffer(buffer, "buffer")
-    e, c, d = shape
-    (n, k), pe, ps = _choices(experts, slots, device)
-    dtype = buffer.dtype
-    code = _code(dtype, "buffer")
-    g, g_stride = _rows(dout, "dout", (n, d), dtype, device)
-    _call("taccl_combine_backward",
-          _CombineBackward(n, c, e, k, d, code, g, g_stride, buffer.data_ptr(), pe, ps,
-                           _flat(counts, "counts", (e,), torch.int32, device),
-                           _flat(weights, "weights", (n, k), torch.float32, device),
-                           _flat(dbuffer, "dbuffer", shape, dtype, device),
-                           _flat(dweights, "dweights", (n, k), torch.float32, device)),
-          device, stream)
+    st = _calls.combine_backward(dout, buffer, experts, slots, counts, weights, dbuffer, dweights,
+                                 stream and stream.cuda_stream)
+    if st:
+        binding._check(st)
 
 
 # ---- differentiable forms ---------------------------------------------------------

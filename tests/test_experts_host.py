@@ -12,14 +12,57 @@ from paper_2111_04867_amd import binding as B
 from paper_2111_04867_amd import experts as X
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-STRUCTS = {"taccl_norm_t": X._Norm, "taccl_norm_backward_t": X._NormBackward,
-           "taccl_route_t": X._Route, "taccl_route_backward_t": X._RouteBackward,
-           "taccl_dispatch_t": X._Dispatch, "taccl_combine_t": X._Combine,
-           "taccl_combine_backward_t": X._CombineBackward}
+_P, _I32, _I64, _F32 = ct.c_void_p, ct.c_int32, ct.c_int64, ct.c_float
+
+
+def _struct(name, fields):
+    return type(name, (ct.Structure,), {"_fields_": fields})
+
+
+# the argument structs of include/taccl.h, in their order
+_Norm = _struct("_Norm", [
+    ("rows", _I64), ("cols", _I32), ("dtype", _I32), ("eps", _F32), ("group", _I32), ("x", _P),
+    ("residual", _P), ("x_stride", _I64), ("residual_stride", _I64), ("weight", _P), ("out", _P),
+    ("total", _P), ("out_stride", _I64), ("total_stride", _I64), ("q", _P), ("scale", _P),
+    ("q_stride", _I64), ("scale_stride", _I64)])
+_NormBackward = _struct("_NormBackward", [
+    ("rows", _I64), ("cols", _I32), ("dtype", _I32), ("eps", _F32), ("dout", _P), ("h", _P),
+    ("dtotal", _P), ("dout_stride", _I64), ("h_stride", _I64), ("dtotal_stride", _I64),
+    ("weight", _P), ("dx", _P), ("dx_stride", _I64), ("dweight", _P), ("workspace", _P),
+    ("workspace_bytes", _I64)])
+_Route = _struct("_Route", [
+    ("tokens", _I64), ("num_experts", _I32), ("k", _I32), ("dtype", _I32), ("renorm", _I32),
+    ("coef", _F32), ("capacity", _I64), ("logits", _P), ("logits_stride", _I64), ("mask", _P),
+    ("experts", _P), ("weights", _P), ("slots", _P), ("counts", _P), ("prob_sums", _P),
+    ("loss", _P), ("rows", _P), ("workspace", _P), ("workspace_bytes", _I64)])
+_RouteBackward = _struct("_RouteBackward", [
+    ("tokens", _I64), ("num_experts", _I32), ("k", _I32), ("dtype", _I32), ("renorm", _I32),
+    ("coef", _F32), ("logits", _P), ("logits_stride", _I64), ("mask", _P), ("experts", _P),
+    ("counts", _P), ("rows", _P), ("dweights", _P), ("dloss", _P), ("dlogits", _P),
+    ("dlogits_stride", _I64)])
+_Dispatch = _struct("_Dispatch", [
+    ("tokens", _I64), ("capacity", _I64), ("num_experts", _I32), ("k", _I32), ("cols", _I32),
+    ("element_bytes", _I32), ("scale_cols", _I32), ("x", _P), ("x_stride", _I64), ("scale", _P),
+    ("scale_stride", _I64), ("experts", _P), ("slots", _P), ("counts", _P), ("out", _P),
+    ("out_scale", _P)])
+_Combine = _struct("_Combine", [
+    ("tokens", _I64), ("capacity", _I64), ("num_experts", _I32), ("k", _I32), ("cols", _I32),
+    ("dtype", _I32), ("buffer", _P), ("experts", _P), ("slots", _P), ("weights", _P), ("out", _P),
+    ("out_stride", _I64)])
+_CombineBackward = _struct("_CombineBackward", [
+    ("tokens", _I64), ("capacity", _I64), ("num_experts", _I32), ("k", _I32), ("cols", _I32),
+    ("dtype", _I32), ("dout", _P), ("dout_stride", _I64), ("buffer", _P), ("experts", _P),
+    ("slots", _P), ("counts", _P), ("weights", _P), ("dbuffer", _P), ("dweights", _P)])
+
+
+STRUCTS = {"taccl_norm_t": _Norm, "taccl_norm_backward_t": _NormBackward,
+           "taccl_route_t": _Route, "taccl_route_backward_t": _RouteBackward,
+           "taccl_dispatch_t": _Dispatch, "taccl_combine_t": _Combine,
+           "taccl_combine_backward_t": _CombineBackward}
 
 
 def test_structs_match_the_header(tmp_path):
-    """Every field of the binding's structs lies where a C compiler puts it."""
+    """Every field of the structs above lies where a C compiler puts it."""
     lines = []
     for name, cls in STRUCTS.items():
         lines.append(f'printf("{name} %zu\\n", sizeof({name}));')
@@ -136,10 +179,10 @@ def test_null_arguments(name):
 
 def test_nothing_to_do():
     """No rows: success without a device."""
-    assert status("taccl_norm", X._Norm(rows=0, cols=4, out=4096))[0] == B.OK
-    assert status("taccl_combine", X._Combine(tokens=0, capacity=1, num_experts=1, k=1,
+    assert status("taccl_norm", _Norm(rows=0, cols=4, out=4096))[0] == B.OK
+    assert status("taccl_combine", _Combine(tokens=0, capacity=1, num_experts=1, k=1,
                                               cols=4))[0] == B.OK
-    assert status("taccl_route_backward", X._RouteBackward(tokens=0, num_experts=4, k=1))[0] == B.OK
+    assert status("taccl_route_backward", _RouteBackward(tokens=0, num_experts=4, k=1))[0] == B.OK
 
 
 def test_binding_refuses_host_tensors_and_wrong_shapes():
@@ -171,3 +214,13 @@ def test_chunk_bytes():
 def test_header_states_the_limits():
     text = open(os.path.join(ROOT, "include", "taccl.h")).read()
     assert re.search(r"1 <= cols <= 16384", text) and re.search(r"tokens <= 2\^21", text)
+
+
+def test_binding_refuses_what_is_no_tensor():
+    x = torch.zeros(4, 8)
+    with pytest.raises(ValueError, match="x must be a CUDA tensor"):
+        X.norm_tensors([1.0], x)
+    with pytest.raises(ValueError, match="buffer must be a CUDA tensor"):
+        X.combine_tensors(None, x, x, x)
+    with pytest.raises(TypeError, match="takes 10 arguments"):
+        X._calls.norm(x)
