@@ -43,6 +43,7 @@ struct RoutePartial {
   float *sums;       // [blocks][wide]
   uint32_t *rows;    // [blocks]
   uint16_t *counts;  // [blocks][wide]
+  unsigned long long *loss;  // the finishing blocks' shares of the loss
   int wide;
   int per_block;  // tokens per block
   int blocks;
@@ -354,6 +355,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
   for (int i = 0; i < kEpl; i++) acc[i] = 0;
   const int64_t begin = (int64_t)blockIdx.x * part.per_block;
   const int64_t end = min(begin + part.per_block, a.tokens);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *part.loss = 0;  // for the second launch
   // a tile's logits are on their way while the one before is worked on
   typedef TokenRow<T, kL, kEpl> Row;
   typename Row::Raw next;
@@ -470,7 +472,8 @@ struct ColumnSums {
   int wide, parts, slices;
   Sk s;
 
-  __device__ __forceinline__ void add(const V *from, int n, int w) {
+  // of the `w` columns at `from`, in rows `stride` values apart
+  __device__ __forceinline__ void add(const V *from, int n, int w, int stride) {
     wide = w;
     parts = w / kN;  // vectors per row, at most 256
     slices = min(kRouteThreads / parts, 32);  // finish() reads them in turn
@@ -482,7 +485,7 @@ struct ColumnSums {
     for (int i = slice; i < n; i += kLoads * slices) {
       Vk x[kLoads];
 #pragma unroll
-      for (int j = 0; j < kLoads; j++) x[j] = p[(int64_t)min(i + j * slices, n - 1) * parts];
+      for (int j = 0; j < kLoads; j++) x[j] = p[(int64_t)min(i + j * slices, n - 1) * (stride / kN)];
 #pragma unroll
       for (int j = 0; j < kLoads; j++)
         if (i + j * slices < n) s += __builtin_convertvector(x[j], Sk);
@@ -501,32 +504,53 @@ struct ColumnSums {
 };
 
 // Second launch: block b adds the counts of the blocks before b to the
-// places of b's choices; the block behind them finishes the totals. Each
-// loads what it needs at once: a round trip to memory is the larger part of
-// its time. The last block takes longest, 3 us for what one CU reads of 256
-// blocks and experts; dealt out over eight blocks, the fences that their totals
-// need took 6 us more than that saved.
+// places of b's choices. The blocks behind them total kFinishCols experts
+// each (one block for all 256 of them takes 3 us for what its CU has to read,
+// 8 instead of 6 us in all). Their shares of the loss, in [0, E], meet in one
+// 64-bit word: 48 bits of them as whole numbers of 2^-37, whose sum does not
+// depend on the order, 8 bits that count shares that are NaN and 8 that count
+// blocks, so that whoever adds the last one holds the loss. Each block loads
+// what it needs at once: a round trip to memory is the larger part of its time.
+constexpr int kFinishCols = 32;
+
 __global__ __launch_bounds__(kRouteThreads) void route_places_kernel(taccl_route_t a,
                                                                      RoutePartial part) {
   __shared__ __align__(16) uint32_t lds[8 * kRouteThreads];
   __shared__ uint32_t cnt[kMaxExperts];
-  __shared__ float sums[kMaxExperts];
-  __shared__ float red[kRouteThreads / 64];
-  const int b = blockIdx.x;
+  const int b = blockIdx.x, wide = part.wide;
   ColumnSums<uint16_t, 8, uint32_t, 8> counts;
-  if (b == part.blocks) {
-    ColumnSums<float, 4, float, 16> probs;
+  if (b >= part.blocks) {
+    __shared__ float sums[kFinishCols];
+    const int first = (b - part.blocks) * kFinishCols, cols = min(kFinishCols, wide - first);
+    ColumnSums<float, 4, float, 8> probs;
     uint32_t n = threadIdx.x < part.blocks ? part.rows[threadIdx.x] : 0;
-    probs.add(part.sums, part.blocks, part.wide);
-    counts.add(part.counts, b, part.wide);
+    counts.add(part.counts + first, part.blocks, cols, wide);
+    probs.add(part.sums + first, part.blocks, cols, wide);
     counts.finish(lds, cnt);
     probs.finish((float *)lds, sums);
     n = wave_scan_add(n);
     if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = n;
     __syncthreads();
+    if (threadIdx.x >= 64) return;
     n = 0;
     for (int w = 0; w < kRouteThreads / 64; w++) n += lds[w];
-    finish_loss(a, cnt, sums, n, red);
+    const int c = threadIdx.x, e = first + c;
+    float s = 0;
+    if (c < cols && e < a.num_experts) {
+      a.counts[e] = (int32_t)cnt[c];
+      a.prob_sums[e] = sums[c];
+      s = (float)cnt[c] * sums[c];
+    }
+    s = lanes_sum<64>(s);
+    if (threadIdx.x) return;
+    const float rows = (float)max(n, 1u);
+    s = s / (rows * (float)a.k) / rows * (float)a.num_experts;
+    const unsigned long long mine =
+        s != s ? 1ull << 8 | 1 : (unsigned long long)((double)s * 0x1p37) << 16 | 1;
+    const unsigned long long all = atomicAdd(part.loss, mine) + mine;
+    if ((int)(all & 0xFF) != (int)gridDim.x - part.blocks) return;
+    *a.loss = all & 0xFF00 ? __builtin_nanf("") : a.coef * (float)((double)(all >> 16) * 0x1p-37);
+    *a.rows = (int32_t)n;
     return;
   }
   const int64_t begin = (int64_t)b * part.per_block * a.k;
@@ -534,7 +558,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_places_kernel(taccl_route
   int64_t i = begin + threadIdx.x;
   int e = i < end ? a.experts[i] : -1;
   int local = i < end ? a.slots[i] : 0;
-  counts.add(part.counts, b, part.wide);
+  counts.add(part.counts, b, wide, wide);
   counts.finish(lds, cnt);
   while (i < end) {
     if (e >= 0) {
@@ -682,10 +706,11 @@ hipError_t launch_route(const taccl_route_t &a, hipStream_t stream) {
   part.sums = (float *)a.workspace;
   part.rows = (uint32_t *)(part.sums + (int64_t)kRouteMaxBlocks * part.wide);
   part.counts = (uint16_t *)(part.rows + kRouteMaxBlocks);
+  part.loss = (unsigned long long *)(part.counts + (int64_t)kRouteMaxBlocks * part.wide);
   void *args[] = {(void *)&a, &part};
   hipError_t e = hipLaunchKernel(fn, dim3(part.blocks), dim3(threads), args, 0, stream);
   if (e != hipSuccess || part.blocks == 1) return e;
-  return hipLaunchKernel((const void *)route_places_kernel, dim3(part.blocks + 1),
+  return hipLaunchKernel((const void *)route_places_kernel, dim3(part.blocks + (part.wide + kFinishCols - 1) / kFinishCols),
                          dim3(kRouteThreads), args, 0, stream);
 }
 
