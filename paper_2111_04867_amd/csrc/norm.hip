@@ -12,9 +12,9 @@
 // with residual and 8-bit copy (303 MB): 512 threads 59.9 us (5.05 TB/s, the
 // rate of a large copy), 256 threads with two vectors 63.5 us, 128 with four
 // 68.4 us, a wavefront with eight 80.6 us: what counts is wavefronts in flight.
-// Gradient: four vectors per thread, so that a block of two to four rows needs
+// Gradient: four vectors per thread, so that a block of two to eight rows needs
 // few partial sums of dw, and 16-bit rows stay as they are stored (as_stored).
-// 8192 x 2048 bf16: 31.1 us for both launches (134 MB; 27 us the first), a
+// 8192 x 2048 bf16: 29.9 us for both launches (134 MB; 26 us the first), a
 // block per row 36 us; 8192 x 4096: 55.1 us with 128 threads per row, 58 us
 // with 256, 71 us with a wavefront.
 #include <hip/hip_runtime.h>
@@ -32,6 +32,11 @@ constexpr float kF8Max = 448.0f;
 constexpr float kAmaxMin = 0x1p-100f;
 
 constexpr int block_threads(int tpr) { return tpr > 256 ? tpr : 256; }
+// The gradient's blocks: eight rows at a time where a wavefront takes one, one
+// block per CU (31.1 us for 8192 x 2048 bf16 with two blocks of four rows, 29.9
+// so); wider rows two blocks of 256 threads (8192 x 4096: 55.1 us, 57.4 with one
+// of 512).
+constexpr int back_threads(int tpr) { return tpr <= 64 || tpr > 256 ? 512 : 256; }
 
 // Sum of v, and maximum of m, over the kTpr threads of a row. `red`: two
 // floats per wavefront; rows in turn alternate between two of them, so one
@@ -168,10 +173,10 @@ __global__ __launch_bounds__(block_threads(kTpr)) void norm_kernel(taccl_norm_t 
 // vector in pieces, behind branches among the loads, took 4 us more for 3001
 // rows of 1999 columns.
 template <class T, int kTpr, int kNv, bool kTail>
-__global__ __launch_bounds__(block_threads(kTpr)) void norm_backward_kernel(
+__global__ __launch_bounds__(back_threads(kTpr)) void norm_backward_kernel(
     taccl_norm_backward_t a, float *partial) {
-  constexpr int N = Vec<T>::kN, kRows = block_threads(kTpr) / kTpr;
-  __shared__ float red[2][2 * (block_threads(kTpr) / 64)];
+  constexpr int N = Vec<T>::kN, kRows = back_threads(kTpr) / kTpr;
+  __shared__ float red[2][2 * (back_threads(kTpr) / 64)];
   constexpr int kCols = kTpr * kNv * N;
   __shared__ __align__(16) float sums[kRows > 1 ? kRows * kCols : 1];
   __shared__ float tail[kRows][N];
@@ -397,9 +402,9 @@ hipError_t launch_norm(const taccl_norm_t &a, hipStream_t stream) {
 hipError_t launch_norm_backward(const taccl_norm_backward_t &a, int cus, hipStream_t stream) {
   RowShape s;
   const void *fn = norm_pick(a.dtype, a.cols, true, s);
-  const int threads = block_threads(s.tpr), per = threads / s.tpr;
+  const int threads = back_threads(s.tpr), per = threads / s.tpr;
   const int grid = (int)std::max<int64_t>(
-      1, std::min<int64_t>({(a.rows + per - 1) / per, (int64_t)cus * 2, kNormMaxBlocks}));
+      1, std::min<int64_t>({(a.rows + per - 1) / per, (int64_t)cus * (s.tpr <= 64 ? 1 : 2), kNormMaxBlocks}));
   float *partial = grid == 1 ? a.dweight : (float *)a.workspace;
   void *args[] = {(void *)&a, &partial};
   hipError_t e = hipLaunchKernel(fn, dim3(grid), dim3(threads), args, 0, stream);
