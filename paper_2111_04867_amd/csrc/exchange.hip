@@ -11,9 +11,9 @@
 //
 // Measured, against 5.09 TB/s of a large copy:
 //   dispatch of 16384 rows of 4096 bytes and 32 scales to 8 of 128 experts, 1280
-//   rows each (762 MB): 147 us, 5.2 TB/s;
+//   rows each (762 MB): 148 us, 5.1 TB/s;
 //   combine of 8192 x 8 rows of 4096 bf16 (604 MB at most): 111 us, 5.4 TB/s;
-//   its gradient, 8192 x 6 rows of 2048 bf16 (487 MB): 104 us, 4.7 TB/s.
+//   its gradient, 8192 x 6 rows of 2048 bf16 (487 MB): 102 us, 4.8 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -9,12 +9,12 @@
 // bytes each. Both kernels are bound by memory.
 //
 // Forward: one vector per thread as far as a block reaches. 8192 x 4096 bf16
-// with residual and 8-bit copy (303 MB): 512 threads 59.9 us (5.05 TB/s, the
-// rate of a large copy), 256 threads with two vectors 63.5 us, 128 with four
+// with residual and 8-bit copy (303 MB): 512 threads 58 us (5.2 TB/s, the rate
+// of a large copy), 256 threads with two vectors 63.5 us, 128 with four
 // 68.4 us, a wavefront with eight 80.6 us: what counts is wavefronts in flight.
 // Gradient: four vectors per thread, so that a block of two to eight rows needs
 // few partial sums of dw, and 16-bit rows stay as they are stored (as_stored).
-// 8192 x 2048 bf16: 29.9 us for both launches (134 MB; 26 us the first), a
+// 8192 x 2048 bf16: 29.4 us for both launches (134 MB; 25.6 us the first), a
 // block per row 36 us; 8192 x 4096: 55.1 us with 128 threads per row, 58 us
 // with 256, 71 us with a wavefront.
 #include <hip/hip_runtime.h>

@@ -13,11 +13,11 @@
 // block and one launch.
 //
 // What bounds it: 32768 tokens, 256 experts, 8 choices, f32 (33.5 MB, 7 us of
-// memory) take 17 us in the first launch, half of them vector instructions
-// (1150 per wavefront, that is for eight tokens), and 8 us in the second, which
-// is mostly launch and round trips to memory. 64 experts, 4 choices: 9 and 5.5
-// us. Taking the k maxima one after the other was 23 us where the threshold
-// below takes 17. The gradient (67 MB, 13 us of memory) takes 22 us.
+// memory) take 15 us in the first launch, half of them vector instructions
+// (1100 per wavefront, that is for eight tokens), and 5.5 us in the second,
+// which is mostly launch and round trips to memory; 64 experts and 4 choices 8.4
+// and 5.2 us. Taking the k maxima one after the other was 23 us where the
+// threshold below takes 15. The gradient (67 MB, 13 us of memory) takes 22 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

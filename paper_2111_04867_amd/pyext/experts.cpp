@@ -1,6 +1,7 @@
 // Argument checks of the expert-layer calls (include/taccl.h) on torch tensors,
 // and the calls. In Python the checks took longer than the launch: 4.2 us of a
-// 7.7 us call for the norm of one token, here 0.5 us.
+// 7.7 us call for the norm of one token (3.5 the launch); with them here a call
+// takes 4.0 us.
 //
 // Functions take positional arguments; None leaves an optional tensor out. The
 // last argument is a hipStream_t, or None for the device's current stream. They
