@@ -68,16 +68,17 @@ struct TokenRow {
   struct Raw {
     W w[kSlots];
     __device__ __forceinline__ void load(const T *row, int lane, int E, bool take) {
+      if (E == kL * kEpl && take) {
+#pragma unroll
+        for (int s = 0; s < kSlots; s++) w[s] = *(const U *)(row + index(lane, s * kN));
+        return;
+      }
 #pragma unroll
       for (int s = 0; s < kSlots; s++)
 #pragma unroll
         for (int x = 0; x < kN; x++) w[s][x] = (T)-__builtin_inff();
       if (!take) return;
-      if (E == kL * kEpl) {
-#pragma unroll
-        for (int s = 0; s < kSlots; s++) w[s] = *(const U *)(row + index(lane, s * kN));
-        return;
-      }
+      asm volatile("" : "+v"(lane));  // its comparisons are not made ahead for the other path
 #pragma unroll
       for (int s = 0; s < kSlots; s++) {
         const int e = index(lane, s * kN);
@@ -100,23 +101,37 @@ struct TokenRow {
 
   // Softmax: the lane's maximum and the exponent's offset (0 in a row of minus
   // infinities and NaNs); the exponentials and 1 / their sum, 0 in a row
-  // without a number.
+  // without a number. The exponent's product with log2(e) and the offset's are
+  // one fused operation: the rounding of the offset's is the same factor in the
+  // whole row and cancels in p. Offsets whose product could overflow go the
+  // other way.
   float top, base, inv;
+  bool huge;
   float p[kEpl];  // exp(v - base)
+  __device__ __forceinline__ float power(float logit) const {
+    constexpr float kLog2e = 1.4426950408889634f;
+    return __builtin_amdgcn_exp2f(huge ? (logit - base) * kLog2e
+                                       : fmaf(logit, kLog2e, -base * kLog2e));
+  }
   __device__ __forceinline__ void maxima() {
     top = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < kEpl; i++) top = fmaxf(top, v[i]);
     const float m = lanes_max<kL>(top);
     base = m == -__builtin_inff() ? 0.0f : m;
+    huge = __any(fabsf(base) > 1e38f);
   }
   __device__ __forceinline__ void exponentials() {
     float s = 0;
+    if (huge) {
 #pragma unroll
-    for (int i = 0; i < kEpl; i++) {
-      p[i] = __expf(v[i] - base);
-      s += p[i];
+      for (int i = 0; i < kEpl; i++) p[i] = power(v[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kEpl; i++) p[i] = power(v[i]);
     }
+#pragma unroll
+    for (int i = 0; i < kEpl; i++) s += p[i];
     s = lanes_sum<kL>(s);
     inv = s == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(s);  // within one unit in the last place
   }
@@ -342,7 +357,10 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
   float (*sums)[kCols] = stage;
   __shared__ float red[kWaves];
   __shared__ uint16_t list[kRanked ? kRouteThreads / kL : 1][16 + 1];
-  __shared__ int16_t picked[kStep * kMaxChoices];  // expert of every choice of the step
+  // the step's choices and weights: written to memory when it is done, since a
+  // store between the tiles would have the next tile's logits wait for it
+  __shared__ int16_t picked[kStep * kMaxChoices];
+  __shared__ float weighed[kStep * kMaxChoices];
   const int E = a.num_experts, k = a.k;
   const int lane = threadIdx.x % kL, group = threadIdx.x / kL, groups = blockDim.x / kL;
   for (int e = threadIdx.x; e <= E; e += blockDim.x) {
@@ -387,7 +405,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
       if (listed) rank_listed<T>(c, n_listed, lane);
       else c = choose_each(x, k, lane);
       const int expert = c.rank < k ? c.expert : -1;
-      float weight = expert >= 0 ? __expf(c.logit - x.base) : 0.0f;
+      float weight = expert >= 0 ? x.power(c.logit) : 0.0f;
       if (a.renorm) {
         const float s = lanes_sum<kL>(weight);
         weight *= s == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(s);
@@ -398,9 +416,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
       if (expert >= 0) atomicOr((unsigned long long *)&bits[expert][at >> 6], bit);
       if (lane == 0 && x.inv != 0.0f) atomicOr((unsigned long long *)&bits[E][at >> 6], bit);
       if (inside && c.rank < k) {
-        a.experts[t * k + c.rank] = expert;
-        a.weights[t * k + c.rank] = weight;
         picked[at * k + c.rank] = (int16_t)expert;
+        weighed[at * k + c.rank] = weight;
       }
     }
     __syncthreads();
@@ -413,6 +430,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
         for (int w = 0; w < word; w++) place += (uint32_t)__popcll(bits[e][w]);
         slot = part.blocks > 1 || !a.capacity || place < a.capacity ? (int)place : -1;
       }
+      a.experts[first * k + i] = e;
+      a.weights[first * k + i] = weighed[i];
       a.slots[first * k + i] = slot;
     }
     __syncthreads();
@@ -614,7 +633,7 @@ __global__ __launch_bounds__(kBackThreads) void route_backward_kernel(taccl_rout
     x.maxima();
     x.exponentials();
     if (a.dweights) {
-      weight = expert >= 0 ? __expf(weight - x.base) : 0.0f;
+      weight = expert >= 0 ? x.power(weight) : 0.0f;
       float term = dw;
       if (a.renorm) {
         const float s = lanes_sum<kL>(weight);
