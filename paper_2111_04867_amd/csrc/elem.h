@@ -130,10 +130,8 @@ __device__ __forceinline__ float lanes_max(float v) {
   v = fmaxf(v, dppf<kRor4>(v));
   v = fmaxf(v, dppf<kRor2>(v));
   v = fmaxf(v, dppf<kRor1>(v));
-  if (L == 64) {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    v = fmaxf(v, __shfl_xor(v, 32));
-  }
+  if (L >= 32) v = fmaxf(v, __shfl_xor(v, 16));
+  if (L == 64) v = fmaxf(v, __shfl_xor(v, 32));
   return v;
 }
 template <int L>
@@ -142,10 +140,8 @@ __device__ __forceinline__ uint32_t lanes_min(uint32_t v) {
   v = min(v, (uint32_t)dppi<kRor4>((int)v));
   v = min(v, (uint32_t)dppi<kRor2>((int)v));
   v = min(v, (uint32_t)dppi<kRor1>((int)v));
-  if (L == 64) {
-    v = min(v, (uint32_t)__shfl_xor((int)v, 16));
-    v = min(v, (uint32_t)__shfl_xor((int)v, 32));
-  }
+  if (L >= 32) v = min(v, (uint32_t)__shfl_xor((int)v, 16));
+  if (L == 64) v = min(v, (uint32_t)__shfl_xor((int)v, 32));
   return v;
 }
 

@@ -11,8 +11,8 @@
 //
 // Measured, against 5.09 TB/s of a large copy:
 //   dispatch of 16384 rows of 4096 bytes and 32 scales to 8 of 128 experts, 1280
-//   rows each (762 MB): 148 us, 5.1 TB/s;
-//   combine of 8192 x 8 rows of 4096 bf16 (604 MB at most): 111 us, 5.4 TB/s;
+//   rows each (762 MB): 147 us, 5.2 TB/s;
+//   combine of 8192 x 8 rows of 4096 bf16 (604 MB at most): 109 us, 5.5 TB/s;
 //   its gradient, 8192 x 6 rows of 2048 bf16 (487 MB): 102 us, 4.8 TB/s.
 #include <hip/hip_runtime.h>
 
@@ -89,6 +89,44 @@ __device__ __forceinline__ void zero_rows(uint8_t *out, const RowUnits &r, const
   if (part == 0 && threadIdx.x == 0) *(Bits16u *)(p + n - 16) = zero;
 }
 
+// The rows of token t's choices, the same in all `lanes` threads of its group.
+// From 16 threads on (kMaxChoices) thread j reads choice j and hands the row to
+// the others: every thread reading every choice made most of a short row's
+// memory instructions (18934 rows of 704 bytes to 7 experts each: 41 us, 33 so;
+// combine of 32768 x 7 rows of 352 bf16: 48 and 42 us).
+template <int kK, class A>
+__device__ __forceinline__ void choice_rows(const A &a, int64_t t, int lanes, int64_t *rows) {
+  if (lanes < kMaxChoices) {
+#pragma unroll
+    for (int j = 0; j < kK; j++)
+      rows[j] = j < a.k ? choice_row(a.experts[t * a.k + j], a.slots[t * a.k + j], a.num_experts,
+                                     a.capacity)
+                        : -1;
+    return;
+  }
+  const int lane = threadIdx.x & (min(lanes, 64) - 1), first = (threadIdx.x & 63) - lane;
+  int64_t own = -1;
+  if (lane < a.k)
+    own = choice_row(a.experts[t * a.k + lane], a.slots[t * a.k + lane], a.num_experts, a.capacity);
+#pragma unroll
+  for (int j = 0; j < kK; j++) rows[j] = __shfl(own, first + j);
+}
+
+// The weights of token t's choices alike (1 without weights, 0 past the k-th)
+template <int kK>
+__device__ __forceinline__ void choice_weights(const float *weights, int k, int64_t t, int lanes,
+                                               float *w) {
+  if (lanes < kMaxChoices) {
+#pragma unroll
+    for (int j = 0; j < kK; j++) w[j] = j >= k ? 0.0f : weights ? weights[t * k + j] : 1.0f;
+    return;
+  }
+  const int lane = threadIdx.x & (min(lanes, 64) - 1), first = (threadIdx.x & 63) - lane;
+  const float own = lane >= k ? 0.0f : weights ? weights[t * k + lane] : 1.0f;
+#pragma unroll
+  for (int j = 0; j < kK; j++) w[j] = __shfl(own, first + j);
+}
+
 struct DispatchArgs {
   taccl_dispatch_t a;
   RowUnits row, scale;
@@ -112,13 +150,13 @@ __global__ __launch_bounds__(kThreads) void dispatch_kernel(DispatchArgs g) {
   const int64_t t = (int64_t)blockIdx.x * per + threadIdx.x / g.lanes;
   if (t >= a.tokens) return;
   int64_t to[kK];
-#pragma unroll
-  for (int j = 0; j < kK; j++)
-    to[j] = j < a.k ? choice_row(a.experts[t * a.k + j], a.slots[t * a.k + j], a.num_experts,
-                                 a.capacity)
-                    : -1;
+  choice_rows<kK>(a, t, g.lanes, to);
   const uint8_t *x = (const uint8_t *)a.x + t * a.x_stride * a.element_bytes;
   uint8_t *out = (uint8_t *)a.out;
+  // the scales' first units are on their way while the row is written
+  const uint8_t *scale = (const uint8_t *)(a.scale + t * a.scale_stride);
+  Bits16 first = {0, 0, 0, 0};
+  if (lane < g.scale.n) first = load_unit(scale + unit_at(g.scale, lane), g.scale.unit);
   if (g.row.unit == 16) {
     for (int u0 = lane; u0 < g.row.n; u0 += kUnits * g.lanes) {
       Bits16 v[kUnits];
@@ -146,7 +184,7 @@ __global__ __launch_bounds__(kThreads) void dispatch_kernel(DispatchArgs g) {
   }
   for (int u = lane; u < g.scale.n; u += g.lanes) {
     const int64_t at = unit_at(g.scale, u);
-    const Bits16 v = load_unit((const uint8_t *)(a.scale + t * a.scale_stride) + at, g.scale.unit);
+    const Bits16 v = u == lane ? first : load_unit(scale + at, g.scale.unit);
 #pragma unroll
     for (int j = 0; j < kK; j++)
       if (to[j] >= 0) store_unit((uint8_t *)a.out_scale + to[j] * g.scale.bytes + at, v, g.scale.unit);
@@ -167,13 +205,8 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs g) {
   if (t >= a.tokens) return;
   int64_t from[kK];
   float w[kK];
-#pragma unroll
-  for (int j = 0; j < kK; j++) {
-    from[j] = j < a.k ? choice_row(a.experts[t * a.k + j], a.slots[t * a.k + j], a.num_experts,
-                                   a.capacity)
-                      : -1;
-    w[j] = j < a.k && a.weights ? a.weights[t * a.k + j] : 1.0f;
-  }
+  choice_rows<kK>(a, t, g.lanes, from);
+  choice_weights<kK>(a.weights, a.k, t, g.lanes, w);
   for (int u = lane; u * N < D; u += g.lanes) {
     const int c = kShort ? 0 : min(u * N, D - N);
     float s[N];
@@ -219,14 +252,10 @@ __global__ __launch_bounds__(kThreads) void combine_backward_kernel(CombineBackw
   if (kWaves == 1 && t >= a.tokens) return;  // else a block is one token
   int64_t at[kK];
   float w[kK], dot[kK];
+  choice_rows<kK>(a, t, kLanes, at);
+  choice_weights<kK>(a.weights, a.k, t, kLanes, w);
 #pragma unroll
-  for (int j = 0; j < kK; j++) {
-    at[j] = j < a.k ? choice_row(a.experts[t * a.k + j], a.slots[t * a.k + j], a.num_experts,
-                                 a.capacity)
-                    : -1;
-    w[j] = j < a.k ? a.weights[t * a.k + j] : 0.0f;
-    dot[j] = 0;
-  }
+  for (int j = 0; j < kK; j++) dot[j] = 0;
   for (int u = lane; u * N < D; u += kLanes) {
     const int c = kShort ? 0 : min(u * N, D - N), twice = u * N - c;
     const auto d = load_vec<T, kShort>((const T *)a.dout + t * a.dout_stride + c, D - c);

@@ -43,7 +43,7 @@ constexpr int back_threads(int tpr) { return tpr <= 64 || tpr > 256 ? 512 : 256;
 // barrier per row is enough.
 template <int kTpr, bool kMax>
 __device__ __forceinline__ void row_reduce(float &v, float &m, float *red) {
-  constexpr int L = kTpr < 64 ? 16 : 64;
+  constexpr int L = kTpr < 64 ? kTpr : 64;
   v = lanes_sum<L>(v);
   if (kMax) m = lanes_max<L>(m);
   else m = lanes_sum<L>(m);
@@ -335,6 +335,7 @@ template <class T>
 RowShape row_shape(int cols, bool backward) {
   const int v = (cols + Vec<T>::kN - 1) / Vec<T>::kN;
   if (v <= 16) return {16, 1};
+  if (v <= 32) return {32, 1};
   if (v <= 64) return {64, 1};
   if (backward) {
     if (v <= 128) return {64, 2};
@@ -356,7 +357,7 @@ template <class T, bool kTail>
 const void *norm_fn(RowShape s) {
 #define PICK(TPR, NV) \
   if (s.tpr == TPR && s.nv == NV) return (const void *)norm_kernel<T, TPR, NV, kTail>;
-  PICK(16, 1) PICK(64, 1) PICK(128, 1) PICK(256, 1) PICK(512, 1) PICK(1024, 1) PICK(1024, 2)
+  PICK(16, 1) PICK(32, 1) PICK(64, 1) PICK(128, 1) PICK(256, 1) PICK(512, 1) PICK(1024, 1) PICK(1024, 2)
   if constexpr (sizeof(T) == 4) {
     PICK(1024, 4)
   }
@@ -367,7 +368,7 @@ template <class T, bool kTail>
 const void *norm_backward_fn(RowShape s) {
 #define PICK(TPR, NV) \
   if (s.tpr == TPR && s.nv == NV) return (const void *)norm_backward_kernel<T, TPR, NV, kTail>;
-  PICK(16, 1) PICK(64, 1) PICK(64, 2) PICK(64, 4) PICK(128, 4) PICK(256, 4) PICK(512, 4)
+  PICK(16, 1) PICK(32, 1) PICK(64, 1) PICK(64, 2) PICK(64, 4) PICK(128, 4) PICK(256, 4) PICK(512, 4)
   if constexpr (sizeof(T) == 4) {
     PICK(512, 8)
   }
