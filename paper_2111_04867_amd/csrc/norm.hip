@@ -75,9 +75,11 @@ __device__ __forceinline__ float group_max(float v, int lanes) {
   return v;
 }
 
-// N floats to e4m3, stored at p (columns from `left` on are not)
-template <int N, bool kTail>
-__device__ __forceinline__ void store_f8(uint8_t *p, const float *y, float inv, int left) {
+// N floats to e4m3, stored at p; only elements first to end - 1 of them where
+// those are not all.
+template <int N, bool kPart>
+__device__ __forceinline__ void store_f8(uint8_t *p, const float *y, float inv, int first,
+                                         int end) {
   uint32_t w[N / 4];
 #pragma unroll
   for (int i = 0; i < N / 4; i++) {
@@ -86,19 +88,26 @@ __device__ __forceinline__ void store_f8(uint8_t *p, const float *y, float inv, 
   }
   typedef uint32_t V __attribute__((ext_vector_type(N / 4)));
   typedef V U __attribute__((aligned(1)));
-  if (left >= N) {
+  if (first == 0 && end >= N) {
     V v;
 #pragma unroll
     for (int i = 0; i < N / 4; i++) v[i] = w[i];
     *(U *)p = v;
-  } else if (kTail) {
+  } else if (kPart) {
 #pragma unroll
     for (int i = 0; i < N; i++)
-      if (i < left) p[i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
+      if (i >= first && i < end) p[i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
   }
 }
 
-template <class T, int kTpr, int kNv, bool kTail>
+// How a row ends: with a whole vector; with one that is moved back to end
+// there, so that its first columns are another thread's too (they count once
+// and are stored twice, alike: reading and writing a last vector in pieces,
+// behind branches, took 7 us more for 8192 rows of 2004 columns); or before the
+// first vector does.
+enum RowEnd { kWhole, kMoved, kShort };
+
+template <class T, int kTpr, int kNv, RowEnd kEnd>
 __global__ __launch_bounds__(block_threads(kTpr)) void norm_kernel(taccl_norm_t a) {
   constexpr int N = Vec<T>::kN, kRows = block_threads(kTpr) / kTpr;
   __shared__ float red[2 * (block_threads(kTpr) / 64)];
@@ -108,27 +117,34 @@ __global__ __launch_bounds__(block_threads(kTpr)) void norm_kernel(taccl_norm_t 
   const int64_t row = live ? at : a.rows - 1;  // rows past the end: computed, not stored
   const T *x = (const T *)a.x + row * a.x_stride;
   const T *res = a.residual ? (const T *)a.residual + row * a.residual_stride : nullptr;
+  // the columns of vector j: from `col`, `left` of them in the row (0: none),
+  // the first `twice` of them the vector's before
+  int col[kNv], left[kNv], twice[kNv];
   float h[kNv][N];
   typename Vec<T>::V wv[kNv];
 #pragma unroll
   for (int j = 0; j < kNv; j++) {
     const int c = N * (lane + kTpr * j);
-    const auto v = load_vec<T, kTail>(x + c, D - c);
+    col[j] = kEnd == kMoved ? min(c, D - N) : c;
+    twice[j] = kEnd == kMoved ? c - col[j] : 0;
+    left[j] = c < D ? D - col[j] : 0;
+    const auto v = load_vec<T, kEnd == kShort>(x + col[j], left[j]);
 #pragma unroll
     for (int i = 0; i < N; i++) h[j][i] = (float)v[i];
     if (res) {
-      const auto r = load_vec<T, kTail>(res + c, D - c);
+      const auto r = load_vec<T, kEnd == kShort>(res + col[j], left[j]);
 #pragma unroll
       for (int i = 0; i < N; i++) h[j][i] += (float)r[i];
     }
-    wv[j] = load_vec<T, kTail>((const T *)a.weight + c, D - c);
+    wv[j] = load_vec<T, kEnd == kShort>((const T *)a.weight + col[j], left[j]);
   }
   float ss = 0, most = 0;
 #pragma unroll
   for (int j = 0; j < kNv; j++)
 #pragma unroll
     for (int i = 0; i < N; i++) {
-      ss += h[j][i] * h[j][i];
+      const float once = kEnd == kMoved && i < twice[j] ? 0.0f : h[j][i];
+      ss += once * once;
       most = fmaxf(most, fabsf(h[j][i] * (float)wv[j][i]));
     }
   row_reduce<kTpr, true>(ss, most, red);
@@ -136,12 +152,12 @@ __global__ __launch_bounds__(block_threads(kTpr)) void norm_kernel(taccl_norm_t 
   const int group = a.group && a.group < D ? a.group : 0;
 #pragma unroll
   for (int j = 0; j < kNv; j++) {
-    const int c = N * (lane + kTpr * j), left = live ? D - c : 0;
+    const int c = col[j], n = live ? left[j] : 0;
     if (a.total) {
       typename Vec<T>::V v;
 #pragma unroll
       for (int i = 0; i < N; i++) v[i] = (T)h[j][i];
-      store_vec<T, kTail>((T *)a.total + row * a.total_stride + c, v, left);
+      store_vec<T, kEnd == kShort>((T *)a.total + row * a.total_stride + c, v, n);
     }
     float y[N];
     typename Vec<T>::V v;
@@ -150,19 +166,24 @@ __global__ __launch_bounds__(block_threads(kTpr)) void norm_kernel(taccl_norm_t 
       y[i] = h[j][i] * r * (float)wv[j][i];
       v[i] = (T)y[i];
     }
-    if (a.out) store_vec<T, kTail>((T *)a.out + row * a.out_stride + c, v, left);
+    if (a.out) store_vec<T, kEnd == kShort>((T *)a.out + row * a.out_stride + c, v, n);
     if (a.q) {
+      const int c0 = N * (lane + kTpr * j);
       float m = most * r;
+      int first = 0;
       if (group) {
         m = 0;
 #pragma unroll
-        for (int i = 0; i < N; i++) m = fmaxf(m, fabsf(y[i]));
+        for (int i = 0; i < N; i++)
+          m = fmaxf(m, kEnd == kMoved && i < twice[j] ? 0.0f : fabsf(y[i]));
         m = group_max(m, group / N);
+        // columns of the group before keep their own scale
+        if (kEnd == kMoved && c0 % group == 0) first = twice[j];
       }
       m = fminf(fmaxf(m, kAmaxMin), 3.4028234664e38f);
-      store_f8<N, kTail>(a.q + row * a.q_stride + c, y, kF8Max / m, left);
-      if (group ? left > 0 && c % group == 0 : live && c == 0)
-        a.scale[row * a.scale_stride + (group ? c / group : 0)] = m / kF8Max;
+      store_f8<N, kEnd != kWhole>(a.q + row * a.q_stride + c, y, kF8Max / m, first, n);
+      if (group ? n > 0 && c0 % group == 0 : live && c0 == 0)
+        a.scale[row * a.scale_stride + (group ? c0 / group : 0)] = m / kF8Max;
     }
   }
 }
@@ -353,10 +374,14 @@ RowShape row_shape(int cols, bool backward) {
   return {1024, 4};  // 32-bit rows only
 }
 
-template <class T, bool kTail>
-const void *norm_fn(RowShape s) {
-#define PICK(TPR, NV) \
-  if (s.tpr == TPR && s.nv == NV) return (const void *)norm_kernel<T, TPR, NV, kTail>;
+template <class T>
+const void *norm_fn(RowShape s, int cols) {
+  if (cols < Vec<T>::kN) return (const void *)norm_kernel<T, 16, 1, kShort>;
+  const bool whole = cols % Vec<T>::kN == 0;
+#define PICK(TPR, NV)                                                            \
+  if (s.tpr == TPR && s.nv == NV)                                                \
+    return whole ? (const void *)norm_kernel<T, TPR, NV, kWhole>                 \
+                 : (const void *)norm_kernel<T, TPR, NV, kMoved>;
   PICK(16, 1) PICK(32, 1) PICK(64, 1) PICK(128, 1) PICK(256, 1) PICK(512, 1) PICK(1024, 1) PICK(1024, 2)
   if constexpr (sizeof(T) == 4) {
     PICK(1024, 4)
@@ -379,8 +404,8 @@ const void *norm_backward_fn(RowShape s) {
 template <class T>
 const void *norm_pick_type(int cols, bool backward, RowShape &s) {
   s = row_shape<T>(cols, backward);
-  if (cols % Vec<T>::kN) return backward ? norm_backward_fn<T, true>(s) : norm_fn<T, true>(s);
-  return backward ? norm_backward_fn<T, false>(s) : norm_fn<T, false>(s);
+  if (!backward) return norm_fn<T>(s, cols);
+  return cols % Vec<T>::kN ? norm_backward_fn<T, true>(s) : norm_backward_fn<T, false>(s);
 }
 
 const void *norm_pick(int dtype, int cols, bool backward, RowShape &s) {
