@@ -1289,6 +1289,6 @@ taccl_status_t taccl_plan_link_costs(taccl_plan_t p, uint32_t *cost_ns) {
 
 const char *taccl_last_error(void) { return taccl::last_error(); }
 
-int32_t taccl_version(void) { return 100; }
+int32_t taccl_version(void) { return 200; }
 
 }  // extern "C"

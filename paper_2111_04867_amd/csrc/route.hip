@@ -263,8 +263,8 @@ __device__ __forceinline__ bool list_ranked(const TokenRow<T, kL, kEpl> &x, int 
   } else {
     float m = x.top, most = m;
     for (int j = 0; j < k; j++) {  // the lanes' maxima, one lane after the other
-      most = lanes_max<64>(m);
-      const uint64_t same = __ballot(m == most);
+      most = lanes_max<kL>(m);
+      const uint64_t same = __ballot(m == most) >> ((threadIdx.x & 63) - lane);
       if (same && lane == __ffsll((unsigned long long)same) - 1) m = -__builtin_inff();
     }
     bound = fmaxf(most, bound);
@@ -275,9 +275,11 @@ __device__ __forceinline__ bool list_ranked(const TokenRow<T, kL, kEpl> &x, int 
 #pragma unroll
   for (int i = 0; i < kEpl; i++) stage[Row::index(lane, i)] = x.v[i];
   const uint32_t mine = __popc(hit);
-  const uint32_t upto = kL == 16 ? row_scan_add(mine) : wave_scan_add(mine);
-  const uint32_t all = kL == 16 ? dpp<0x15F>(upto)  // the row's last lane
-                                : (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+  uint32_t upto = row_scan_add(mine), all;
+  if (kL > 16) upto += dpp<kBcast15, 0xa>(upto);
+  if (kL > 32) upto += dpp<kBcast31, 0xc>(upto);
+  if (kL == 16) all = dpp<0x15F>(upto);  // the group's last lane
+  else all = (uint32_t)__shfl((int)upto, (threadIdx.x & 63) - lane + kL - 1);
   if (__any(all > 16)) return false;
   uint32_t at = upto - mine;
   const uint32_t first = (uint32_t)lane * Row::kN;  // Row::index(lane, 0)
@@ -305,18 +307,21 @@ __device__ __forceinline__ void rank_listed(Choice &c, uint32_t n, int lane) {
   if (c.expert >= 0) c.rank = rank;
 }
 
-// Sums over the wavefront's four rows of 16 lanes, one of four values to each
-// row: the total of v[0], v[2], v[1], v[3] in rows 0 to 3. A swap puts half of
-// two registers into one, so two values are added with one addition.
+// Sums of two registers across the wavefront's halves (rows: across its odd
+// and even rows of 16 lanes), a's in the lower half (even rows) and b's in the
+// upper one. The swap puts half of each register into the other, so one
+// addition does both.
+__device__ __forceinline__ float swapped_sum(float a, float b, bool rows) {
+  const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
+  const auto r = rows ? __builtin_amdgcn_permlane16_swap(x, y, false, false)
+                      : __builtin_amdgcn_permlane32_swap(x, y, false, false);
+  const uint32_t first = r[0], second = r[1];
+  return __uint_as_float(first) + __uint_as_float(second);
+}
+// Sums over the four rows, one of four values to each: the totals of v[0],
+// v[2], v[1], v[3] in rows 0 to 3
 __device__ __forceinline__ float rows_sum(const float *v) {
-  auto pair = [](float a, float b, bool rows) {
-    const uint32_t x = __float_as_uint(a), y = __float_as_uint(b);
-    const auto r = rows ? __builtin_amdgcn_permlane16_swap(x, y, false, false)
-                        : __builtin_amdgcn_permlane32_swap(x, y, false, false);
-    const uint32_t first = r[0], second = r[1];
-    return __uint_as_float(first) + __uint_as_float(second);
-  };
-  return pair(pair(v[0], v[1], false), pair(v[2], v[3], false), true);
+  return swapped_sum(swapped_sum(v[0], v[1], false), swapped_sum(v[2], v[3], false), true);
 }
 
 // The balance loss and the totals from the experts' counts and sums in LDS
@@ -449,6 +454,11 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
   if (kL == 64) {
 #pragma unroll
     for (int i = 0; i < kEpl; i++) mine[Row::index(lane, i)] = acc[i];
+  } else if (kL == 32) {
+    const int upper = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int i = 0; i < kEpl; i += 2)
+      mine[Row::index(lane, i) + upper] = swapped_sum(acc[i], acc[i + 1], false);
   } else {
     const int r = (threadIdx.x & 63) >> 4, turn = (r >> 1) | (r & 1) << 1;  // rows_sum's order
 #pragma unroll
@@ -681,11 +691,12 @@ __global__ __launch_bounds__(kBackThreads) void route_backward_kernel(taccl_rout
   }
 }
 
-// lanes per token and experts per lane: 16 lanes up to 256 experts
+// lanes per token and experts per lane: 16 lanes up to 256 experts, 16 experts
+// from there on (32768 tokens, 300 experts: first launch 25 us, 37 in 64 lanes of 8)
 #define BY_EXPERTS(E, F)                                                                   \
   ((E) <= 16 ? F(16, 1) : (E) <= 32 ? F(16, 2) : (E) <= 64 ? F(16, 4) : (E) <= 128 ? F(16, 8) \
-   : (E) <= 256 ? F(16, 16) : (E) <= 512 ? F(64, 8) : F(64, 16))
-int token_lanes(int E) { return E <= 256 ? 16 : 64; }
+   : (E) <= 256 ? F(16, 16) : (E) <= 512 ? F(32, 16) : F(64, 16))
+int token_lanes(int E) { return E <= 256 ? 16 : E <= 512 ? 32 : 64; }
 
 template <class T>
 const void *route_fn(int E, int k) {
