@@ -13,7 +13,7 @@
 //   dispatch of 16384 rows of 4096 bytes and 32 scales to 8 of 128 experts, 1280
 //   rows each (762 MB): 147 us, 5.2 TB/s;
 //   combine of 8192 x 8 rows of 4096 bf16 (604 MB at most): 109 us, 5.5 TB/s;
-//   its gradient, 8192 x 6 rows of 2048 bf16 (487 MB): 102 us, 4.8 TB/s.
+//   its gradient, 8192 x 6 rows of 2048 bf16 (487 MB): 95 us, 5.1 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -368,9 +368,9 @@ hipError_t launch_combine_backward(const taccl_combine_backward_t &a, int cus,
   CombineBackwardArgs g{a, {}, 0, 1};
   const int size = a.dtype == TACCL_F32 ? 4 : 2;
   g.row = row_units((int64_t)a.cols * size, size);
-  // a unit per lane up to a wavefront; a block where tokens are few and rows long
-  int lanes = std::max(16, row_lanes(g.row.n, 64));
-  if (a.tokens < 4 * (int64_t)cus && g.row.n > 64) lanes = kThreads;
+  // a unit per lane up to a wavefront, a block past two units each (8192 x 6 rows of
+  // 2048 bf16: 103 us with a wavefront, 95 so; 8192 x 4 of 1111 f32: 86 and 76)
+  const int lanes = g.row.n > 128 ? kThreads : std::max(16, row_lanes(g.row.n, 64));
   const int64_t per = kThreads / lanes;
   g.token_blocks = (int)((a.tokens + per - 1) / per);
   g.parts = zero_parts(a.capacity, a.num_experts, cus);
