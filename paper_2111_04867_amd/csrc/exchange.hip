@@ -11,8 +11,8 @@
 //
 // Measured, against 5.09 TB/s of a large copy:
 //   dispatch of 16384 rows of 4096 bytes and 32 scales to 8 of 128 experts, 1280
-//   rows each (762 MB): 147 us, 5.2 TB/s;
-//   combine of 8192 x 8 rows of 4096 bf16 (604 MB at most): 109 us, 5.5 TB/s;
+//   rows each (762 MB): 149 us, 5.1 TB/s;
+//   combine of 8192 x 8 rows of 4096 bf16 (604 MB at most): 108 us, 5.6 TB/s;
 //   its gradient, 8192 x 6 rows of 2048 bf16 (487 MB): 95 us, 5.1 TB/s.
 #include <hip/hip_runtime.h>
 
@@ -187,7 +187,8 @@ __global__ __launch_bounds__(kThreads) void dispatch_kernel(DispatchArgs g) {
     const Bits16 v = u == lane ? first : load_unit(scale + at, g.scale.unit);
 #pragma unroll
     for (int j = 0; j < kK; j++)
-      if (to[j] >= 0) store_unit((uint8_t *)a.out_scale + to[j] * g.scale.bytes + at, v, g.scale.unit);
+      if (to[j] >= 0)
+        store_unit((uint8_t *)a.out_scale + to[j] * g.scale.bytes + at, v, g.scale.unit);
   }
 }
 
@@ -314,7 +315,9 @@ int zero_parts(int64_t capacity, int E, int cus) {
 template <class T>
 const void *combine_fn(int k, int cols) {
   const bool brief = cols < Vec<T>::kN;  // a row shorter than a unit
-#define F(K) (brief ? (const void *)combine_kernel<T, K, true> : (const void *)combine_kernel<T, K, false>)
+#define F(K)                                            \
+  (brief ? (const void *)combine_kernel<T, K, true>     \
+         : (const void *)combine_kernel<T, K, false>)
   return BY_CHOICES(k, F);
 #undef F
 }
@@ -336,7 +339,9 @@ const void *combine_backward_fn(int k, int cols, int lanes) {
 }  // namespace
 
 hipError_t launch_dispatch(const taccl_dispatch_t &a, int cus, hipStream_t stream) {
-  DispatchArgs g{a, row_units((int64_t)a.cols * a.element_bytes, a.element_bytes), {0, 4, 0}, 1, 0, 1};
+  DispatchArgs g{};
+  g.a = a;
+  g.row = row_units((int64_t)a.cols * a.element_bytes, a.element_bytes);
   if (a.scale_cols) g.scale = row_units(4 * (int64_t)a.scale_cols, 4);
   g.lanes = row_lanes(g.row.n, 128);
   const int64_t per = kThreads / g.lanes;

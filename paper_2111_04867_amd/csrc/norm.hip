@@ -14,7 +14,7 @@
 // 68.4 us, a wavefront with eight 80.6 us: what counts is wavefronts in flight.
 // Gradient: four vectors per thread, so that a block of two to eight rows needs
 // few partial sums of dw, and 16-bit rows stay as they are stored (as_stored).
-// 8192 x 2048 bf16: 29.4 us for both launches (134 MB; 25.6 us the first), a
+// 8192 x 2048 bf16: 29.9 us for both launches (134 MB; 25.8 us the first), a
 // block per row 36 us; 8192 x 4096: 55.1 us with 128 threads per row, 58 us
 // with 256, 71 us with a wavefront.
 #include <hip/hip_runtime.h>
@@ -84,7 +84,8 @@ __device__ __forceinline__ void store_f8(uint8_t *p, const float *y, float inv, 
 #pragma unroll
   for (int i = 0; i < N / 4; i++) {
     int x = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i] * inv, y[4 * i + 1] * inv, 0, false);
-    w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2] * inv, y[4 * i + 3] * inv, x, true);
+    x = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2] * inv, y[4 * i + 3] * inv, x, true);
+    w[i] = (uint32_t)x;
   }
   typedef uint32_t V __attribute__((ext_vector_type(N / 4)));
   typedef V U __attribute__((aligned(1)));
@@ -429,8 +430,8 @@ hipError_t launch_norm_backward(const taccl_norm_backward_t &a, int cus, hipStre
   RowShape s;
   const void *fn = norm_pick(a.dtype, a.cols, true, s);
   const int threads = back_threads(s.tpr), per = threads / s.tpr;
-  const int grid = (int)std::max<int64_t>(
-      1, std::min<int64_t>({(a.rows + per - 1) / per, (int64_t)cus * (s.tpr <= 64 ? 1 : 2), kNormMaxBlocks}));
+  const int64_t most = std::min<int64_t>((int64_t)cus * (s.tpr <= 64 ? 1 : 2), kNormMaxBlocks);
+  const int grid = (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + per - 1) / per, most));
   float *partial = grid == 1 ? a.dweight : (float *)a.workspace;
   void *args[] = {(void *)&a, &partial};
   hipError_t e = hipLaunchKernel(fn, dim3(grid), dim3(threads), args, 0, stream);

@@ -13,11 +13,11 @@
 // block and one launch.
 //
 // What bounds it: 32768 tokens, 256 experts, 8 choices, f32 (33.5 MB, 7 us of
-// memory) take 15 us in the first launch, half of them vector instructions
-// (1100 per wavefront, that is for eight tokens), and 5.5 us in the second,
-// which is mostly launch and round trips to memory; 64 experts and 4 choices 8.4
-// and 5.2 us. Taking the k maxima one after the other was 23 us where the
-// threshold below takes 15. The gradient (67 MB, 13 us of memory) takes 22 us.
+// memory) take 14.5 us in the first launch, half of them vector instructions
+// (950 per wavefront, that is for eight tokens), and 5.5 us in the second, which
+// is mostly launch and round trips to memory; 64 experts and 4 choices 8.5 and
+// 5.1 us. Taking the k maxima one after the other was 23 us where the threshold
+// below takes 14.5. The gradient (67 MB, 13 us of memory) takes 22 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -403,7 +403,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
       x.maxima();
       Choice c;
       uint32_t n_listed = 0;
-      const bool listed = kRanked && list_ranked(x, k, lane, stage[group], list[group], c, n_listed);
+      const bool listed =
+          kRanked && list_ranked(x, k, lane, stage[group], list[group], c, n_listed);
       x.exponentials();
 #pragma unroll
       for (int i = 0; i < kEpl; i++) acc[i] += x.p[i] * x.inv;
@@ -415,7 +416,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
         const float s = lanes_sum<kL>(weight);
         weight *= s == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(s);
       } else {
-        weight *= x.inv;
+        weight = expert >= 0 ? weight * x.inv : 0.0f;  // inv may be NaN
       }
       const unsigned long long bit = 1ull << (at & 63);
       if (expert >= 0) atomicOr((unsigned long long *)&bits[expert][at >> 6], bit);
@@ -514,7 +515,8 @@ struct ColumnSums {
     for (int i = slice; i < n; i += kLoads * slices) {
       Vk x[kLoads];
 #pragma unroll
-      for (int j = 0; j < kLoads; j++) x[j] = p[(int64_t)min(i + j * slices, n - 1) * (stride / kN)];
+      for (int j = 0; j < kLoads; j++)
+        x[j] = p[(int64_t)min(i + j * slices, n - 1) * (stride / kN)];
 #pragma unroll
       for (int j = 0; j < kLoads; j++)
         if (i + j * slices < n) s += __builtin_convertvector(x[j], Sk);
@@ -740,7 +742,8 @@ hipError_t launch_route(const taccl_route_t &a, hipStream_t stream) {
   void *args[] = {(void *)&a, &part};
   hipError_t e = hipLaunchKernel(fn, dim3(part.blocks), dim3(threads), args, 0, stream);
   if (e != hipSuccess || part.blocks == 1) return e;
-  return hipLaunchKernel((const void *)route_places_kernel, dim3(part.blocks + (part.wide + kFinishCols - 1) / kFinishCols),
+  const int finish = (part.wide + kFinishCols - 1) / kFinishCols;
+  return hipLaunchKernel((const void *)route_places_kernel, dim3(part.blocks + finish),
                          dim3(kRouteThreads), args, 0, stream);
 }
 

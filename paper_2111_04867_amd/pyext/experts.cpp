@@ -71,7 +71,8 @@ int32_t dtype_code(const Tensor &t, const char *name, bool matrix) {
     if (t.scalar_type() == at::kBFloat16) return TACCL_BF16;
     if (t.scalar_type() == at::kHalf) return TACCL_F16;
   }
-  misfit(t, name, std::string(matrix ? "a matrix" : "a tensor") + " of float32, bfloat16 or float16");
+  misfit(t, name,
+         std::string(matrix ? "a matrix" : "a tensor") + " of float32, bfloat16 or float16");
 }
 
 // The call's device and stream, by the tensor that its others go by

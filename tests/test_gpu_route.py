@@ -136,6 +136,22 @@ def test_nan_logits():
     assert int(got["rows"]) == 6
 
 
+@pytest.mark.parametrize("renorm", [True, False])
+def test_rows_of_nan(renorm):
+    """A row without a number has no choice and weights of 0, whatever its
+    probabilities; one with a single number chooses that."""
+    for e in (12, 100, 300):
+        x = logits_of(5, e, torch.float32, e)
+        x[1] = torch.nan
+        x[3] = torch.nan
+        x[3, 7] = 0.5
+        got = run(x, 3, renorm=renorm)
+        assert (got["experts"][1] == -1).all() and (got["weights"][1] == 0).all()
+        assert got["experts"][3].tolist() == [7, -1, -1]
+        assert (got["weights"][3, 1:] == 0).all()
+        assert (got["slots"][1] == -1).all() and got["loss"].isnan().all()
+
+
 def test_no_tokens():
     got = run(torch.empty(0, 9, device="cuda"), 2)
     assert (got["counts"] == 0).all() and (got["prob_sums"] == 0).all()
