@@ -366,9 +366,10 @@ typedef enum { TACCL_F32 = 0, TACCL_BF16 = 1, TACCL_F16 = 2 } taccl_dtype_t;
  *   out: y; total: h (the next layer's residual; may be `residual` or `x`
  *     itself, with the same stride); q, scale: y in 8 bits (OCP e4m3) with one
  *     scale per `group` columns (32, 64, 128 or 256; 0: one per row),
- *     scale = max(max |y| of the group, 2^-100) / 448 and q = y / scale to
- *     nearest even; a NaN or infinite y is NaN in q and a NaN leaves its
- *     group's scale alone. scale has ceil(cols / group) values per row.
+ *     scale = max(max |y| of the group, 2^-100) / 448 and q = y / scale, the
+ *     quotient in 32 bits and then to nearest even; a NaN or infinite y is NaN
+ *     in q and a NaN leaves its group's scale alone. scale has
+ *     ceil(cols / group) values per row.
  * 1 <= cols <= 16384, rows <= 2^21. rows == 0 is a no-op.
  */
 typedef struct {

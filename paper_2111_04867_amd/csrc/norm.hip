@@ -75,16 +75,17 @@ __device__ __forceinline__ float group_max(float v, int lanes) {
   return v;
 }
 
-// N floats to e4m3, stored at p; only elements first to end - 1 of them where
-// those are not all.
+// N floats over `scale` in e4m3, stored at p; only elements first to end - 1 of
+// them where those are not all. The quotient itself is rounded: a product with
+// the scale's rounded reciprocal is another e4m3 number for 1 value in 1e5.
 template <int N, bool kPart>
-__device__ __forceinline__ void store_f8(uint8_t *p, const float *y, float inv, int first,
+__device__ __forceinline__ void store_f8(uint8_t *p, const float *y, float scale, int first,
                                          int end) {
   uint32_t w[N / 4];
 #pragma unroll
   for (int i = 0; i < N / 4; i++) {
-    int x = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i] * inv, y[4 * i + 1] * inv, 0, false);
-    x = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2] * inv, y[4 * i + 3] * inv, x, true);
+    int x = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i] / scale, y[4 * i + 1] / scale, 0, false);
+    x = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2] / scale, y[4 * i + 3] / scale, x, true);
     w[i] = (uint32_t)x;
   }
   typedef uint32_t V __attribute__((ext_vector_type(N / 4)));
@@ -181,10 +182,10 @@ __global__ __launch_bounds__(block_threads(kTpr)) void norm_kernel(taccl_norm_t 
         // columns of the group before keep their own scale
         if (kEnd == kMoved && c0 % group == 0) first = twice[j];
       }
-      m = fminf(fmaxf(m, kAmaxMin), 3.4028234664e38f);
-      store_f8<N, kEnd != kWhole>(a.q + row * a.q_stride + c, y, kF8Max / m, first, n);
+      const float scale = fminf(fmaxf(m, kAmaxMin), 3.4028234664e38f) / kF8Max;
+      store_f8<N, kEnd != kWhole>(a.q + row * a.q_stride + c, y, scale, first, n);
       if (group ? n > 0 && c0 % group == 0 : live && c0 == 0)
-        a.scale[row * a.scale_stride + (group ? c0 / group : 0)] = m / kF8Max;
+        a.scale[row * a.scale_stride + (group ? c0 / group : 0)] = scale;
     }
   }
 }
