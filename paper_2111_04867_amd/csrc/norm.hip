@@ -38,15 +38,30 @@ constexpr int block_threads(int tpr) { return tpr > 256 ? tpr : 256; }
 // of 512).
 constexpr int back_threads(int tpr) { return tpr <= 64 || tpr > 256 ? 512 : 256; }
 
-// Sum of v, and maximum of m, over the kTpr threads of a row. `red`: two
-// floats per wavefront; rows in turn alternate between two of them, so one
-// barrier per row is enough.
+// Sum or maximum of v over the kTpr threads of a row. `red`: a float per
+// wavefront.
 template <int kTpr, bool kMax>
-__device__ __forceinline__ void row_reduce(float &v, float &m, float *red) {
+__device__ __forceinline__ float row_reduce(float v, float *red) {
+  constexpr int L = kTpr < 64 ? kTpr : 64;
+  v = kMax ? lanes_max<L>(v) : lanes_sum<L>(v);
+  if (kTpr <= 64) return v;
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  red += threadIdx.x / kTpr * (kTpr / 64);
+  v = red[0];
+#pragma unroll
+  for (int i = 1; i < kTpr / 64; i++) v = kMax ? fmaxf(v, red[i]) : v + red[i];
+  return v;
+}
+
+// Sums of v and m over the kTpr threads of a row. `red`: two floats per
+// wavefront; rows in turn alternate between two of them, so one barrier per row
+// is enough.
+template <int kTpr>
+__device__ __forceinline__ void row_sums(float &v, float &m, float *red) {
   constexpr int L = kTpr < 64 ? kTpr : 64;
   v = lanes_sum<L>(v);
-  if (kMax) m = lanes_max<L>(m);
-  else m = lanes_sum<L>(m);
+  m = lanes_sum<L>(m);
   if (kTpr <= 64) return;
   const int w = threadIdx.x >> 6;
   if ((threadIdx.x & 63) == 0) {
@@ -60,7 +75,7 @@ __device__ __forceinline__ void row_reduce(float &v, float &m, float *red) {
 #pragma unroll
   for (int i = 1; i < kTpr / 64; i++) {
     v += red[2 * i];
-    m = kMax ? fmaxf(m, red[2 * i + 1]) : m + red[2 * i + 1];
+    m += red[2 * i + 1];
   }
 }
 
@@ -112,7 +127,7 @@ enum RowEnd { kWhole, kMoved, kShort };
 template <class T, int kTpr, int kNv, RowEnd kEnd>
 __global__ __launch_bounds__(block_threads(kTpr)) void norm_kernel(taccl_norm_t a) {
   constexpr int N = Vec<T>::kN, kRows = block_threads(kTpr) / kTpr;
-  __shared__ float red[2 * (block_threads(kTpr) / 64)];
+  __shared__ float red[2][block_threads(kTpr) / 64];
   const int lane = threadIdx.x % kTpr, D = a.cols;
   const int64_t at = (int64_t)blockIdx.x * kRows + threadIdx.x / kTpr;
   const bool live = at < a.rows;
@@ -140,18 +155,27 @@ __global__ __launch_bounds__(block_threads(kTpr)) void norm_kernel(taccl_norm_t 
     }
     wv[j] = load_vec<T, kEnd == kShort>((const T *)a.weight + col[j], left[j]);
   }
-  float ss = 0, most = 0;
+  float ss = 0;
 #pragma unroll
   for (int j = 0; j < kNv; j++)
 #pragma unroll
     for (int i = 0; i < N; i++) {
       const float once = kEnd == kMoved && i < twice[j] ? 0.0f : h[j][i];
       ss += once * once;
-      most = fmaxf(most, fabsf(h[j][i] * (float)wv[j][i]));
     }
-  row_reduce<kTpr, true>(ss, most, red);
+  ss = row_reduce<kTpr, false>(ss, red[0]);
   const float r = 1.0f / sqrtf(ss / (float)D + a.eps);
   const int group = a.group && a.group < D ? a.group : 0;
+  // one scale per row is by the values themselves: the maximum of h w, taken
+  // with the sum and times r, rounds otherwise and can leave y's range
+  float most = 0;
+  if (a.q && !group) {
+#pragma unroll
+    for (int j = 0; j < kNv; j++)
+#pragma unroll
+      for (int i = 0; i < N; i++) most = fmaxf(most, fabsf(h[j][i] * r * (float)wv[j][i]));
+    most = row_reduce<kTpr, true>(most, red[1]);
+  }
 #pragma unroll
   for (int j = 0; j < kNv; j++) {
     const int c = col[j], n = live ? left[j] : 0;
@@ -171,7 +195,7 @@ __global__ __launch_bounds__(block_threads(kTpr)) void norm_kernel(taccl_norm_t 
     if (a.out) store_vec<T, kEnd == kShort>((T *)a.out + row * a.out_stride + c, v, n);
     if (a.q) {
       const int c0 = N * (lane + kTpr * j);
-      float m = most * r;
+      float m = most;
       int first = 0;
       if (group) {
         m = 0;
@@ -264,7 +288,7 @@ __global__ __launch_bounds__(back_threads(kTpr)) void norm_backward_kernel(
       as_stored(hv[j]);
       as_stored(wv[j]);
     }
-    row_reduce<kTpr, false>(ss, dot, red[turn]);
+    row_sums<kTpr>(ss, dot, red[turn]);
     const float r = 1.0f / sqrtf(ss / (float)D + a.eps);
     const float f = r * r * r * (dot / (float)D);
 #pragma unroll
