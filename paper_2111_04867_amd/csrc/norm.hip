@@ -290,7 +290,9 @@ __global__ __launch_bounds__(back_threads(kTpr)) void norm_backward_kernel(
     }
     row_sums<kTpr>(ss, dot, red[turn]);
     const float r = 1.0f / sqrtf(ss / (float)D + a.eps);
-    const float f = r * r * r * (dot / (float)D);
+    // h r^3 mean(a h) as (h r) (r mean(a h)): the cube leaves the range from rows
+    // of 1e13 (or of 1e-13 without eps) on, these factors stay within it
+    const float f = dot * r / (float)D;
 #pragma unroll
     for (int j = 0; j < kNv; j++) {
       const int c = N * (lane + kTpr * j);
@@ -298,16 +300,18 @@ __global__ __launch_bounds__(back_threads(kTpr)) void norm_backward_kernel(
 #pragma unroll
       for (int i = 0; i < N; i++) {
         const float x = (float)hv[j][i], d = (float)dv[j][i];
-        float g = r * (d * (float)wv[j][i]) - x * f;
+        const float u = x * r;
+        float g = r * (d * (float)wv[j][i] - u * f);
         if (dt) g += (float)tv[j][i];
         o[i] = (T)g;
-        if (live) acc[j][i] += d * (x * r);
+        if (live) acc[j][i] += d * u;
       }
       store_vec<T, false>(dx + c, o, live ? whole - c : 0);
     }
     if (more && live) {
-      dx[whole + lane] = (T)(r * (d1 * w1) - h1 * f + t1);
-      acc1 += d1 * (h1 * r);
+      const float u1 = h1 * r;
+      dx[whole + lane] = (T)(r * (d1 * w1 - u1 * f) + t1);
+      acc1 += d1 * u1;
     }
   }
   float *out = partial + (int64_t)blockIdx.x * D;

@@ -57,3 +57,21 @@ def test_scales_of_small_weights(d, group):
     assert torch.equal(scale.cpu(), row_maxima(out.cpu(), group) / 448)
     want = (out.cpu() / by_column(scale.cpu(), d, group)).to(torch.float8_e4m3fn)
     assert torch.equal(q.cpu().view(torch.uint8), want.view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("size", [1e-17, 1e-15, 1e-13, 1e12, 1e13, 1e15, 1e17])
+@pytest.mark.parametrize("n,d", [(5, 7), (40, 100), (600, 200), (30, 1999), (9, 4096), (3, 16384)])
+def test_backward_of_large_and_small_rows(n, d, size, dtype):
+    """1 / sqrt(mean) cubed leaves the range, the gradient does not. Bounds as
+    for rows of ordinary size."""
+    g = gen(n + d)
+    h = (size * (0.5 + torch.rand(n, d, generator=g, device="cuda"))).to(dtype)
+    dy = torch.randn(n, d, generator=g, device="cuda").to(dtype)
+    w = (1 + 0.1 * torch.randn(d, generator=g, device="cuda")).to(dtype)
+    dx, dw = torch.empty_like(h), torch.empty(d, device="cuda")
+    work = torch.empty(X.norm_workspace(d), dtype=torch.uint8, device="cuda")
+    X.norm_backward_tensors(dy, h, w, dx, dw, work, eps=0.0)
+    want, want_dw, terms, terms_dw = F.norm_backward(dy, h, w, 0.0, None)
+    F.close(dx, want, dtype, 64 * U * terms)
+    F.close(dw, want_dw, torch.float32, (100 + n / 256) * U * terms_dw)
