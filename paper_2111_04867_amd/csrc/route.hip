@@ -101,17 +101,13 @@ struct TokenRow {
 
   // Softmax: the lane's maximum and the exponent's offset (0 in a row of minus
   // infinities and NaNs); the exponentials and 1 / their sum, 0 in a row
-  // without a number. The exponent's product with log2(e) and the offset's are
-  // one fused operation: the rounding of the offset's is the same factor in the
-  // whole row and cancels in p. Offsets whose product could overflow go the
-  // other way.
+  // without a number. The offset is taken off before the product with log2(e):
+  // as fma(logit, log2e, -(offset log2e)) the rounding of the second product
+  // would be a factor of the whole row that overflows from offsets of 1e9 on.
   float top, base, inv;
-  bool huge;
   float p[kEpl];  // exp(v - base)
   __device__ __forceinline__ float power(float logit) const {
-    constexpr float kLog2e = 1.4426950408889634f;
-    return __builtin_amdgcn_exp2f(huge ? (logit - base) * kLog2e
-                                       : fmaf(logit, kLog2e, -base * kLog2e));
+    return __builtin_amdgcn_exp2f((logit - base) * 1.4426950408889634f);
   }
   __device__ __forceinline__ void maxima() {
     top = -__builtin_inff();
@@ -119,19 +115,14 @@ struct TokenRow {
     for (int i = 0; i < kEpl; i++) top = fmaxf(top, v[i]);
     const float m = lanes_max<kL>(top);
     base = m == -__builtin_inff() ? 0.0f : m;
-    huge = __any(fabsf(base) > 1e38f);
   }
   __device__ __forceinline__ void exponentials() {
     float s = 0;
-    if (huge) {
 #pragma unroll
-      for (int i = 0; i < kEpl; i++) p[i] = power(v[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kEpl; i++) p[i] = power(v[i]);
+    for (int i = 0; i < kEpl; i++) {
+      p[i] = power(v[i]);
+      s += p[i];
     }
-#pragma unroll
-    for (int i = 0; i < kEpl; i++) s += p[i];
     s = lanes_sum<kL>(s);
     inv = s == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(s);  // within one unit in the last place
   }
