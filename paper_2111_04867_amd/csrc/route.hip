@@ -404,7 +404,15 @@ __global__ __launch_bounds__(kRouteThreads) void route_kernel(taccl_route_t a, R
       const int expert = c.rank < k ? c.expert : -1;
       float weight = expert >= 0 ? x.power(c.logit) : 0.0f;
       if (a.renorm) {
-        const float s = lanes_sum<kL>(weight);
+        // summed with the j-th choice's in lane j, however the choices were found:
+        // that is up to the wavefront's other tokens, on which a row's bits do not
+        // depend
+        float w = weight;
+        if (listed) {
+          const int to = (int)(threadIdx.x & 63) - lane + c.rank;
+          w = __int_as_float(__builtin_amdgcn_ds_permute(4 * to, __float_as_int(weight)));
+        }
+        const float s = lanes_sum<kL>(w);
         weight *= s == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(s);
       } else {
         weight = expert >= 0 ? weight * x.inv : 0.0f;  // inv may be NaN

@@ -61,6 +61,18 @@ def test_backward(e, k, size, dtype, renorm):
     backward(large_rows(e, dtype, size, 40), k, renorm)
 
 
+@pytest.mark.parametrize("e", [40, 300, 700])
+def test_bits_do_not_depend_on_the_neighbours(e):
+    x = large_rows(e, torch.float32, 1e20, 40)
+    plain = torch.randn(40, e, generator=torch.Generator(device="cuda").manual_seed(1),
+                        device="cuda")
+    a, mixed = run(plain, 4), plain.clone()
+    mixed[1::3] = x[1::3]
+    b = run(mixed, 4)
+    keep = [t for t in range(40) if t % 3 != 1]
+    assert torch.equal(a["weights"][keep], b["weights"][keep])
+
+
 def test_a_batch_with_one_padding_row():
     """Eight equal logits of -1e30: 1/8 each, and nothing of it elsewhere."""
     x = torch.randn(64, 8, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
