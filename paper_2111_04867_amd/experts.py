@@ -11,12 +11,13 @@ the tokens from the rows that come back.
 `stream` (default: torch's current stream) of the current device, without
 allocating; a tensor made on another stream has to be ready on this one, as
 for any kernel. `norm`, `route`, `dispatch` and `combine` allocate their
-results and are differentiable. There is no fallback: without the library they
-raise.
+results and are differentiable, once: a second derivative raises. There is no
+fallback: without the library they raise.
 """
 import ctypes as ct
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding
 
@@ -170,6 +171,7 @@ class _NormFn(torch.autograd.Function):
         return out, (total if residual is not None else None), q, scale
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout, dtotal, _q, _scale):
         h, weight = ctx.saved_tensors
         if dout is None:
@@ -209,6 +211,7 @@ class _RouteFn(torch.autograd.Function):
         return experts, weights, slots, counts, prob_sums, loss, rows
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, _experts, dweights, _slots, _counts, _sums, dloss, _rows_):
         logits, experts, counts, rows = ctx.saved_tensors
         dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
@@ -234,6 +237,7 @@ class _DispatchFn(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         experts, slots = ctx.saved_tensors
         dx = torch.empty(len(experts), dout.shape[2], dtype=dout.dtype, device=dout.device)
@@ -255,6 +259,7 @@ class _CombineFn(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         buffer, experts, slots, counts, weights = ctx.saved_tensors
         dbuffer, dweights = torch.empty_like(buffer), torch.empty_like(weights)

@@ -1,0 +1,42 @@
+"""What autograd may and may not do with the differentiable operators."""
+import pytest
+import torch
+
+from paper_2111_04867_amd import experts as X
+
+pytestmark = pytest.mark.gpu
+
+
+def randn(seed, *shape):
+    return torch.randn(*shape, generator=torch.Generator(device="cuda").manual_seed(seed),
+                       device="cuda")
+
+
+def routed():
+    return X.route(randn(1, 20, 6), 2, capacity=9)
+
+
+@pytest.mark.parametrize("op", ["norm", "route", "dispatch", "combine", "combine_weights"])
+def test_second_derivatives_are_refused(op):
+    """A gradient penalty that also reaches its input another way has a second
+    derivative without the operator's part; it raises."""
+    experts, weights, slots, counts = (routed()[i] for i in (0, 1, 2, 3))
+    x = randn(2, 9 * 6 if op == "combine" else 20, 8)
+    if op == "route":
+        x = randn(1, 20, 6)
+    if op == "combine_weights":
+        x = weights
+    x = x.detach().requires_grad_()
+    if op == "norm":
+        out = X.norm(x, torch.ones(8, device="cuda"))[0]
+    elif op == "route":
+        out = X.route(x, 2)[1]
+    elif op == "dispatch":
+        out = X.dispatch(x, experts, slots, counts, 9)
+    elif op == "combine":
+        out = X.combine(x.view(6, 9, 8), experts, slots, counts, weights)
+    else:
+        out = X.combine(randn(3, 6, 9, 8), experts, slots, counts, x)
+    g, = torch.autograd.grad((out ** 3).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="twice|once_differentiable"):
+        (g * x).sum().backward()
