@@ -205,20 +205,20 @@ class _RouteFn(torch.autograd.Function):
         route_tensors(logits, experts, weights, slots, counts, prob_sums, loss, rows,
                       _workspace(route_workspace(e), logits), mask=mask, capacity=capacity,
                       coef=coef, renorm=renorm)
-        ctx.save_for_backward(logits, experts, counts, rows)
-        ctx.mask, ctx.coef, ctx.renorm = mask, coef, renorm
+        ctx.save_for_backward(logits, experts, counts, rows, mask)
+        ctx.coef, ctx.renorm = coef, renorm
         ctx.mark_non_differentiable(experts, slots, counts, prob_sums, rows)
         return experts, weights, slots, counts, prob_sums, loss, rows
 
     @staticmethod
     @once_differentiable
     def backward(ctx, _experts, dweights, _slots, _counts, _sums, dloss, _rows_):
-        logits, experts, counts, rows = ctx.saved_tensors
+        logits, experts, counts, rows, mask = ctx.saved_tensors
         dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
         route_backward_tensors(logits, experts, counts, rows, dlogits,
                                dweights=None if dweights is None else dweights.contiguous(),
                                dloss=None if dloss is None else dloss.contiguous(),
-                               mask=ctx.mask, coef=ctx.coef, renorm=ctx.renorm)
+                               mask=mask, coef=ctx.coef, renorm=ctx.renorm)
         return dlogits, None, None, None, None, None
 
 

@@ -40,3 +40,14 @@ def test_second_derivatives_are_refused(op):
     g, = torch.autograd.grad((out ** 3).sum(), x, create_graph=True)
     with pytest.raises(RuntimeError, match="twice|once_differentiable"):
         (g * x).sum().backward()
+
+
+def test_mask_written_between_the_passes():
+    """The gradient needs the forward pass's mask: a changed one raises."""
+    x = randn(1, 30, 8).requires_grad_()
+    mask = torch.ones(30, dtype=torch.uint8, device="cuda")
+    mask[::3] = 0
+    loss = X.route(x, 2, mask=mask)[5]
+    mask.fill_(1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.sum().backward()
