@@ -96,7 +96,7 @@ def route_tensors(logits, experts, weights, slots, counts, prob_sums, loss, rows
                   mask=None, capacity=0, coef=0.01, renorm=True, stream=None):
     """taccl_route: experts int32, weights float32 and slots int32
     [tokens, k], counts int32 and prob_sums float32 [experts], loss float32
-    [1] and rows int32 [1] from logits [tokens, experts]; mask uint8 [tokens]."""
+    [1] and rows int32 [1] from logits [tokens, experts]; mask uint8 or bool [tokens]."""
     st = _calls.route(logits, experts, weights, slots, counts, prob_sums, loss, rows, workspace,
                       mask, capacity, coef, renorm, stream and stream.cuda_stream)
     if st:

@@ -131,6 +131,12 @@ struct At {
     p = (P *)t.data_ptr();
   }
 
+  // a mask: a byte per token, or a truth value
+  void mask(PyObject *o, int64_t n, const uint8_t *&p) const {
+    const bool truth = THPVariable_Check(o) && THPVariable_Unpack(o).scalar_type() == at::kBool;
+    flat(o, "mask", {n}, truth ? at::kBool : at::kByte, p);
+  }
+
   void workspace(PyObject *o, void *&p, int64_t &bytes) const {
     const Tensor &t = tensor(o, "workspace");
     if (t.get_device() != device || !t.is_contiguous())
@@ -250,7 +256,7 @@ PyObject *route(PyObject *const *o) {
   at.flat(o[6], "loss", {1}, at::kFloat, a.loss);
   at.flat(o[7], "rows", {1}, at::kInt, a.rows);
   at.workspace(o[8], a.workspace, a.workspace_bytes);
-  at.flat(o[9], "mask", {n}, at::kByte, a.mask);
+  at.mask(o[9], n, a.mask);
   a.capacity = whole(o[10]);
   a.coef = (float)real(o[11]);
   a.renorm = PyObject_IsTrue(o[12]);
@@ -276,7 +282,7 @@ PyObject *route_backward(PyObject *const *o) {
   at.rows(o[4], "dlogits", n, e, l.scalar_type(), a.dlogits, a.dlogits_stride);
   at.flat(o[5], "dweights", {n, k}, at::kFloat, a.dweights);
   at.flat(o[6], "dloss", {1}, at::kFloat, a.dloss);
-  at.flat(o[7], "mask", {n}, at::kByte, a.mask);
+  at.mask(o[7], n, a.mask);
   a.coef = (float)real(o[8]);
   a.renorm = PyObject_IsTrue(o[9]);
   return run(route_backward_fn, a, at);

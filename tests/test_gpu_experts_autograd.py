@@ -51,3 +51,21 @@ def test_mask_written_between_the_passes():
     mask.fill_(1)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.sum().backward()
+
+
+@pytest.mark.parametrize("renorm", [True, False])
+def test_boolean_mask(renorm):
+    """The same as its bytes, in both passes."""
+    got = []
+    for dtype in (torch.uint8, torch.bool):
+        x = randn(1, 300, 12).requires_grad_()
+        mask = (torch.arange(300, device="cuda") % 4 != 1).to(dtype)
+        out = X.route(x, 3, mask=mask, capacity=50, renorm=renorm)
+        ((out[1] * randn(2, 300, 3)).sum() + out[5].sum()).backward()
+        got.append([*out, x.grad])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    with pytest.raises(ValueError, match="mask"):
+        X.route(x, 3, mask=mask.float())
+    with pytest.raises(ValueError, match="mask"):
+        X.route(x, 3, mask=torch.ones(600, dtype=torch.bool, device="cuda")[::2])
