@@ -262,7 +262,11 @@ class _CombineFn(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dout):
         buffer, experts, slots, counts, weights = ctx.saved_tensors
-        dbuffer, dweights = torch.empty_like(buffer), torch.empty_like(weights)
+        dbuffer = torch.empty_like(buffer)
+        if weights is None:
+            dispatch_tensors(_gradient_rows(dout), experts, slots, counts, dbuffer)
+            return dbuffer, None, None, None, None
+        dweights = torch.empty_like(weights)
         combine_backward_tensors(_gradient_rows(dout), buffer, experts, slots, counts, weights,
                                  dbuffer, dweights)
         return dbuffer, None, None, None, dweights
@@ -270,5 +274,5 @@ class _CombineFn(torch.autograd.Function):
 
 def combine(buffer, experts, slots, counts, weights):
     """Tokens [tokens, dim] of combine_tensors; gradients flow to the buffer
-    and the weights."""
+    and the weights (None: 1)."""
     return _CombineFn.apply(buffer, experts, slots, counts, weights)

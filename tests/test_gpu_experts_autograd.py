@@ -69,3 +69,18 @@ def test_boolean_mask(renorm):
         X.route(x, 3, mask=mask.float())
     with pytest.raises(ValueError, match="mask"):
         X.route(x, 3, mask=torch.ones(600, dtype=torch.bool, device="cuda")[::2])
+
+
+def test_combine_without_weights():
+    """Weights of 1, and their gradient left out."""
+    experts, weights, slots, counts = (routed()[i] for i in (0, 1, 2, 3))
+    got = []
+    for w in (None, torch.ones_like(weights)):
+        buffer = randn(3, 6, 9, 8).requires_grad_()
+        out = X.combine(buffer, experts, slots, counts, w)
+        (out * randn(4, 20, 8)).sum().backward()
+        got.append((out, buffer.grad))
+    assert torch.equal(got[0][0], got[1][0])
+    used = torch.arange(9, device="cuda") < counts[:, None]
+    assert int((~used).sum()) > 0 and (got[0][1][~used] == 0).all()
+    assert torch.equal(got[0][1], got[1][1])
