@@ -8,7 +8,9 @@
 // raise ValueError for tensors that do not fit and return the library's status.
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <initializer_list>
+#include <limits>
 #include <sstream>
 #include <stdexcept>
 #include <string>
@@ -73,6 +75,12 @@ int32_t dtype_code(const Tensor &t, const char *name, bool matrix) {
   }
   misfit(t, name,
          std::string(matrix ? "a matrix" : "a tensor") + " of float32, bfloat16 or float16");
+}
+
+// A size in the call's 32 bits. One that does not fit stays past every limit
+// there instead of coming out as another size.
+int32_t size32(int64_t n) {
+  return (int32_t)std::min<int64_t>(n, std::numeric_limits<int32_t>::max());
 }
 
 // The call's device and stream, by the tensor that its others go by
@@ -152,7 +160,7 @@ void choices(A &a, const At &at, PyObject *experts, PyObject *slots) {
   const Tensor &e = tensor(experts, "experts");
   if (e.dim() != 2) misfit(e, "experts", "a matrix [tokens, k]");
   a.tokens = e.size(0);
-  a.k = (int32_t)e.size(1);
+  a.k = size32(e.size(1));
   at.flat(experts, "experts", {a.tokens, a.k}, at::kInt, a.experts);
   at.flat(slots, "slots", {a.tokens, a.k}, at::kInt, a.slots);
 }
@@ -165,9 +173,9 @@ const Tensor &buffer(PyObject *o, const char *name) {
 }
 template <class A>
 void buffer_sizes(A &a, const Tensor &t) {
-  a.num_experts = (int32_t)t.size(0);
+  a.num_experts = size32(t.size(0));
   a.capacity = t.size(1);
-  a.cols = (int32_t)t.size(2);
+  a.cols = size32(t.size(2));
 }
 
 double real(PyObject *o) {
@@ -203,7 +211,7 @@ PyObject *norm(PyObject *const *o) {
   const ScalarType type = x.scalar_type();
   const At at(x, "x", o[9]);
   const int64_t n = a.rows = x.size(0), d = x.size(1);
-  a.cols = (int32_t)d;
+  a.cols = size32(d);
   a.eps = (float)real(o[3]);
   a.group = small(o[8], "group");
   at.rows(x, "x", n, d, type, a.x, a.x_stride);
@@ -225,7 +233,7 @@ PyObject *norm_backward(PyObject *const *o) {
   const ScalarType type = h.scalar_type();
   const At at(h, "h", o[8]);
   const int64_t n = a.rows = h.size(0), d = h.size(1);
-  a.cols = (int32_t)d;
+  a.cols = size32(d);
   a.eps = (float)real(o[6]);
   at.rows(h, "h", n, d, type, a.h, a.h_stride);
   at.rows(o[0], "dout", n, d, type, a.dout, a.dout_stride);
@@ -245,7 +253,7 @@ PyObject *route(PyObject *const *o) {
   a.dtype = dtype_code(l, "logits", true);
   const At at(l, "logits", o[13]);
   const int64_t n = l.size(0), e = l.size(1);
-  a.num_experts = (int32_t)e;
+  a.num_experts = size32(e);
   choices(a, at, o[1], o[3]);
   a.tokens = n;
   at.rows(l, "logits", n, e, l.scalar_type(), a.logits, a.logits_stride);
@@ -270,11 +278,11 @@ PyObject *route_backward(PyObject *const *o) {
   a.dtype = dtype_code(l, "logits", true);
   const At at(l, "logits", o[10]);
   const int64_t n = a.tokens = l.size(0), e = l.size(1);
-  a.num_experts = (int32_t)e;
+  a.num_experts = size32(e);
   const Tensor &experts = tensor(o[1], "experts");
   if (experts.dim() != 2) misfit(experts, "experts", "a matrix [tokens, k]");
   const int64_t k = experts.size(1);
-  a.k = (int32_t)k;
+  a.k = size32(k);
   at.rows(l, "logits", n, e, l.scalar_type(), a.logits, a.logits_stride);
   at.flat(o[1], "experts", {n, k}, at::kInt, a.experts);
   at.flat(o[2], "counts", {e}, at::kInt, a.counts);
@@ -303,7 +311,7 @@ PyObject *dispatch(PyObject *const *o) {
     const Tensor &scale = tensor(o[5], "scale");
     if (scale.dim() != 2) misfit(scale, "scale", "a matrix [tokens, n]");
     tensor(o[6], "out_scale");
-    a.scale_cols = (int32_t)scale.size(1);
+    a.scale_cols = size32(scale.size(1));
     at.rows(scale, "scale", a.tokens, a.scale_cols, at::kFloat, a.scale, a.scale_stride);
     at.flat(o[6], "out_scale", {a.num_experts, a.capacity, a.scale_cols}, at::kFloat, a.out_scale);
   }

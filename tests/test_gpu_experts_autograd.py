@@ -84,3 +84,24 @@ def test_combine_without_weights():
     used = torch.arange(9, device="cuda") < counts[:, None]
     assert int((~used).sum()) > 0 and (got[0][1][~used] == 0).all()
     assert torch.equal(got[0][1], got[1][1])
+
+
+def test_sizes_past_32_bits():
+    """Columns, experts and choices whose low 32 bits alone would pass are
+    refused, not cut. No array holds anything but the weight (8.6 GB, not
+    touched): there are no rows."""
+    d = (1 << 32) + 64
+    x = torch.empty(0, d, dtype=torch.float16, device="cuda")
+    w = torch.empty(d, dtype=torch.float16, device="cuda")
+    with pytest.raises(X.binding.TacclError, match="more than 16384 columns"):
+        X.norm_tensors(x, w, x)
+    del w
+    none = torch.empty(0, 2, dtype=torch.int32, device="cuda")
+    with pytest.raises(X.binding.TacclError, match="more than 1024 experts"):
+        X.combine_tensors(torch.empty((1 << 32) + 4, 0, 8, device="cuda"), none, none,
+                          torch.empty(0, 8, device="cuda"))
+    many = torch.empty(0, (1 << 32) + 2, dtype=torch.int32, device="cuda")
+    with pytest.raises((ValueError, X.binding.TacclError), match="choices"):
+        X.route_backward_tensors(torch.empty(0, 8, device="cuda"), many, *(
+            torch.zeros(s, dtype=torch.int32, device="cuda") for s in (8, 1)),
+            torch.empty(0, 8, device="cuda"))
