@@ -37,10 +37,12 @@ def back(received, ranks):
     return [b.view(-1, *b.shape[2:]) for b in sent]
 
 
+GROUP = 128  # columns per scale of an 8-bit row
+
+
 def rows_in_floats(q, scale):
     """8-bit rows with their scales as bfloat16."""
-    n = q.shape[-1]
-    wide = scale.repeat_interleave(-(-n // scale.shape[-1]), dim=-1)[..., :n]
+    wide = scale.repeat_interleave(GROUP, dim=-1)[..., :q.shape[-1]]
     return (q.float() * wide).bfloat16()
 
 
@@ -57,7 +59,7 @@ def layer(hidden, residual, model, k, capacity, ranks, eight_bits=False):
     """(tokens out, residual out, balance loss, counts) of every rank."""
     sent, scales, kept = [], [], []
     for x, r in zip(hidden, residual):
-        y, total, q, scale = X.norm(x, model["norm"], r, quantize=eight_bits)
+        y, total, q, scale = X.norm(x, model["norm"], r, group=GROUP, quantize=eight_bits)
         logits = (y @ model["router"]).float()
         experts, weights, slots, counts, _, loss, _ = X.route(logits, k, capacity=capacity)
         if eight_bits:
@@ -114,7 +116,7 @@ def main(tokens=1024, dim=1024, num_experts=64, k=4, steps=30, candidates=2048, 
         out8 = layer(hidden, residual, model, k, capacity, ranks, eight_bits=True)[0]
     off = max(((a.float() - b.float()).norm() / b.float().norm()).item() for a, b in zip(out8, out))
     times = {}
-    for name, row in (("16-bit rows", 2 * dim), ("8-bit rows", dim + 4 * -(-dim // 128))):
+    for name, row in (("16-bit rows", 2 * dim), ("8-bit rows", dim + 4 * -(-dim // GROUP))):
         chunk = X.chunk_bytes(num_experts, capacity, row, ranks)
         times[name] = best_schedule(chunk, candidates)
         say(f"{name}: chunks of {chunk} bytes, best of {candidates} schedules "
@@ -131,7 +133,7 @@ def main(tokens=1024, dim=1024, num_experts=64, k=4, steps=30, candidates=2048, 
             model["router"] -= 0.3 * g / g.norm() * dim ** 0.5 / steps ** 0.5
             model["router"].grad = None
     last = dropped(counts, even * 5 // 4)
-    chunk = X.chunk_bytes(num_experts, even * 5 // 4, dim + 4 * -(-dim // 128), ranks)
+    chunk = X.chunk_bytes(num_experts, even * 5 // 4, dim + 4 * -(-dim // GROUP), ranks)
     times["evened"] = best_schedule(chunk, candidates)
     say(f"choices past 1.25 times the even load: {first:.3f} before and {last:.3f} after {steps} "
         f"steps; with that capacity {times['evened']:.1f} us")
