@@ -355,7 +355,9 @@ taccl_status_t taccl_generate_host(taccl_plan_t plan, uint64_t seed, int64_t fir
  * (to nearest even). Errors (synchronous): INVALID_ARGUMENT for null
  * pointers, negative sizes, strides below the row's length, misaligned
  * pointers or unknown types, LIMIT for sizes beyond the stated ones, HIP if
- * a launch fails.
+ * a launch fails. The router's exponentials and reciprocals are the device's
+ * own (within a unit in the last place; a power below 2^-126 may be 0),
+ * divisions and square roots are rounded to nearest.
  * ------------------------------------------------------------------------ */
 typedef enum { TACCL_F32 = 0, TACCL_BF16 = 1, TACCL_F16 = 2 } taccl_dtype_t;
 
@@ -367,9 +369,13 @@ typedef enum { TACCL_F32 = 0, TACCL_BF16 = 1, TACCL_F16 = 2 } taccl_dtype_t;
  *     itself, with the same stride); q, scale: y in 8 bits (OCP e4m3) with one
  *     scale per `group` columns (32, 64, 128 or 256; 0: one per row),
  *     scale = max(max |y| of the group, 2^-100) / 448 and q = y / scale, the
- *     quotient in 32 bits and then to nearest even; a NaN or infinite y is NaN
- *     in q and a NaN leaves its group's scale alone. scale has
- *     ceil(cols / group) values per row.
+ *     quotient in 32 bits and then to nearest even (of 16-bit rows 5 in 1e5
+ *     quotients are ties but for the roundings of y and scale, and go either
+ *     way); a NaN or infinite y is NaN in q and a NaN leaves its group's scale
+ *     alone. scale has ceil(cols / group) values per row.
+ * The sum of h^2 is held in 32 bits: where it is infinite (a value of 2e19, or
+ * 4096 of 3e17) y is 0; where it is 0 without eps (values of 1e-23) y is infinite
+ * or NaN.
  * 1 <= cols <= 16384, rows <= 2^21. rows == 0 is a no-op.
  */
 typedef struct {
@@ -393,8 +399,8 @@ taccl_status_t taccl_norm(const taccl_norm_t *a, taccl_stream_t stream);
  * Gradient of y (above) with respect to h, which x and residual share, and
  * to the weight, for h as given (the stored total):
  *   r = 1 / sqrt(mean(h^2) + eps), a = weight * dout,
- *   dx = dtotal + r * a - h * r^3 * mean(a * h),  dweight = sum over rows of
- *   dout * h * r (32-bit floats; zero without rows).
+ *   dx = dtotal + r * (a - h * r * mean(a * h * r)),  dweight = sum over rows
+ *   of dout * h * r (32-bit floats; zero without rows).
  * dx may be dout, dtotal or h itself, with the same stride. `workspace`:
  * taccl_norm_workspace(cols) bytes, 16-byte aligned, not shared with another
  * call in flight.
@@ -493,7 +499,10 @@ taccl_status_t taccl_route_backward(const taccl_route_backward_t *a, taccl_strea
  * the buffer has none. 1 <= E <= 1024, 1 <= k <= 16, 1 <= capacity < 2^31,
  * tokens <= 2^21, 1 <= cols <= 2^20. Offsets in the buffer are 64-bit.
  *
- * Dispatch: out[row of (t, j)] = x[t], and rows from counts[e] on are zero.
+ * Dispatch: out[row of (t, j)] = x[t], and rows from counts[e] on are zero. A
+ * row below counts[e] that no choice has (where the router's capacity is below
+ * the buffer's, or a choice was taken out) is left as it is, here and in the
+ * gradient of combine: counts limited to the router's capacity make it zero.
  * Elements of 1, 2 or 4 bytes; with the scales of 8-bit rows, scale
  * [tokens][scale_cols] goes to out_scale [E][capacity][scale_cols] alike.
  */

@@ -11,9 +11,10 @@
 //
 // Measured, against 5.09 TB/s of a large copy:
 //   dispatch of 16384 rows of 4096 bytes and 32 scales to 8 of 128 experts, 1280
-//   rows each (762 MB): 149 us, 5.1 TB/s;
-//   combine of 8192 x 8 rows of 4096 bf16 (604 MB at most): 108 us, 5.6 TB/s;
-//   its gradient, 8192 x 6 rows of 2048 bf16 (487 MB): 95 us, 5.1 TB/s.
+//   rows each (762 MB): 148 us, 5.1 TB/s;
+//   combine of 8192 x 8 rows of 4096 bf16, less those past the capacity (537 MB
+//   by the counters): 111 us, 4.9 TB/s;
+//   its gradient, 8192 x 6 rows of 2048 bf16 alike (453 MB): 94 us, 4.8 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -15,7 +15,7 @@ constexpr int kNormMaxBlocks = 1024;  // partial rows of dweight in the workspac
 constexpr int kMaxExperts = 1024;
 constexpr int kMaxChoices = 16;
 constexpr int kRouteMaxBlocks = 256;  // partial counts and sums in the workspace
-// a grid has fewer than 2^32 threads, up to 512 of them per row
+// a grid has fewer than 2^32 threads, up to 1024 of them per row
 constexpr int64_t kMaxRows = 1 << 21;
 constexpr int kExchangeMaxCols = 1 << 20;
 

@@ -159,7 +159,9 @@ taccl_status_t taccl_norm_backward(const taccl_norm_backward_t *a, taccl_stream_
 }
 
 int64_t taccl_route_workspace(int32_t num_experts) {
-  const int64_t wide = ((int64_t)num_experts + 7) / 8 * 8;  // rows of 6 bytes each, and a count
+  // per block a row of sums (4 bytes each), one of counts (2) and the tokens that
+  // count (4), and the word of the loss (8): it lies in the 2 bytes per column to spare
+  const int64_t wide = ((int64_t)num_experts + 7) / 8 * 8;
   return num_experts < 1 ? 0 : kRouteMaxBlocks * (8 * wide + 4);
 }
 

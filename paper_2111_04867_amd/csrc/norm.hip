@@ -2,21 +2,23 @@
 // copy, and its gradient.
 //
 //   h = x + residual, r = 1 / sqrt(mean(h^2) + eps), y = w h r
-//   dx = dtotal + r a - h r^3 mean(a h) with a = w dy;  dw = sum_t dy h r
+//   dx = dtotal + r (a - u mean(a u)) with a = w dy, u = h r;  dw = sum_t dy u
 //
 // A row is held in registers between its two passes (statistics, outputs), so
 // memory is read and written once: kTpr threads per row, kNv vectors of 16
 // bytes each. Both kernels are bound by memory.
 //
 // Forward: one vector per thread as far as a block reaches. 8192 x 4096 bf16
-// with residual and 8-bit copy (303 MB): 512 threads 58 us (5.2 TB/s, the rate
-// of a large copy), 256 threads with two vectors 63.5 us, 128 with four
-// 68.4 us, a wavefront with eight 80.6 us: what counts is wavefronts in flight.
+// with residual and 8-bit copy (303 MB): 57 us a call (5.3 TB/s; a large copy
+// 5.1), vector instructions busy 90% of it, most of them the divisions of the
+// 8-bit copy. 512 threads took 58 us where 256 with two vectors took 63.5, 128
+// with four 68.4 and a wavefront with eight 80.6 (with products by a reciprocal
+// in the divisions' place): what counts is wavefronts in flight.
 // Gradient: four vectors per thread, so that a block of two to eight rows needs
 // few partial sums of dw, and 16-bit rows stay as they are stored (as_stored).
-// 8192 x 2048 bf16: 29.9 us for both launches (134 MB; 25.8 us the first), a
-// block per row 36 us; 8192 x 4096: 55.1 us with 128 threads per row, 58 us
-// with 256, 71 us with a wavefront.
+// 8192 x 2048 bf16: 29.7 us for both launches (134 MB; in a trace 27.0 us the
+// first and 4.6 the second, on average), a block per row 36 us; 8192 x 4096: 55.9
+// us with 128 threads per row, where 256 took 3 us more and a wavefront 16.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -92,7 +94,8 @@ __device__ __forceinline__ float group_max(float v, int lanes) {
 
 // N floats over `scale` in e4m3, stored at p; only elements first to end - 1 of
 // them where those are not all. The quotient itself is rounded: a product with
-// the scale's rounded reciprocal is another e4m3 number for 1 value in 1e5.
+// the scale's rounded reciprocal is another e4m3 number for 1 in 2e6 values of
+// 32-bit rows and for 1 in 1e5 of 16-bit ones, which have more ties.
 template <int N, bool kPart>
 __device__ __forceinline__ void store_f8(uint8_t *p, const float *y, float scale, int first,
                                          int end) {

@@ -12,12 +12,13 @@
 // through floating atomics, so their order is fixed; a small batch takes one
 // block and one launch.
 //
-// What bounds it: 32768 tokens, 256 experts, 8 choices, f32 (33.5 MB, 7 us of
-// memory) take 14.5 us in the first launch, half of them vector instructions
-// (950 per wavefront, that is for eight tokens), and 5.5 us in the second, which
-// is mostly launch and round trips to memory; 64 experts and 4 choices 8.5 and
-// 5.1 us. Taking the k maxima one after the other was 23 us where the threshold
-// below takes 14.5. The gradient (67 MB, 13 us of memory) takes 22 us.
+// What bounds it (averages of a trace): 32768 tokens, 256 experts, 8 choices, f32
+// (33.5 MB, 7 us of memory) take 16.0 us in the first launch, half of them vector
+// instructions (980 per wavefront, that is for eight tokens), and 5.9 us in the
+// second, which is mostly launch and round trips to memory; 64 experts and 4
+// choices 8.3 and 5.3 us. Taking the k maxima one after the other took 1.5 times
+// the threshold's time. The gradient (69 MB, 14 us of memory) takes 21.5 us: the
+// chosen logits are read where the choices, read before them, say.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -33,8 +34,8 @@ constexpr int kRouteThreads = 1024;
 constexpr int kBackThreads = 256;
 // up to kSmallTile tokens a block of 256 threads, up to kOneBlock one of 1024
 // (two launches: 11.6 instead of 9 us), up to kSmallBlocks blocks of 256 again,
-// so that the tokens are spread over the CUs (6000 tokens, 64 experts: 11.9 us,
-// 13.1 with 1024)
+// so that the tokens are spread over the CUs (6000 tokens, 64 experts: 11.0 us a
+// call for both launches, about one more with 1024)
 constexpr int kSmallTile = 16, kOneBlock = 128, kSmallBlocks = 8192;
 
 // Per-block results: the experts' counts and probability sums in rows padded
@@ -536,7 +537,7 @@ struct ColumnSums {
 // Second launch: block b adds the counts of the blocks before b to the
 // places of b's choices. The blocks behind them total kFinishCols experts
 // each (one block for all 256 of them takes 3 us for what its CU has to read,
-// 8 instead of 6 us in all). Their shares of the loss, in [0, E], meet in one
+// 8 instead of 5.9 us in all). Their shares of the loss, in [0, E], meet in one
 // 64-bit word: 48 bits of them as whole numbers of 2^-37, whose sum does not
 // depend on the order, 8 bits that count shares that are NaN and 8 that count
 // blocks, so that whoever adds the last one holds the loss. Each block loads

@@ -246,7 +246,9 @@ class _DispatchFn(torch.autograd.Function):
 
 
 def dispatch(x, experts, slots, counts, capacity):
-    """Buffer [experts, capacity, dim] of dispatch_tensors."""
+    """Buffer [experts, capacity, dim] of dispatch_tensors. `capacity` is
+    route's, or less; for a larger buffer give counts.clamp(max=route's), here
+    and to combine, or the rows between hold whatever the memory held."""
     return _DispatchFn.apply(x, experts, slots, counts, capacity)
 
 
