@@ -553,6 +553,141 @@ typedef struct {
 } taccl_combine_backward_t;
 taccl_status_t taccl_combine_backward(const taccl_combine_backward_t *a, taccl_stream_t stream);
 
+/*
+ * The experts themselves: gated feed-forward of the rows in a buffer
+ * [sources][E][capacity][cols]. sources is 1 for the buffer that dispatch
+ * fills, or the number of ranks whose rows an Alltoall put together (each
+ * rank's part as it arrives, E the rank's own experts); counts[s][e] rows of
+ * source s go to expert e (more than capacity: capacity; negative: 0), which
+ * may be the router's counts. For an expert's row x
+ *   g = Wg x, u = Wu x, a = silu(g) * u, y = Wo a,  silu(g) = g / (1 + exp(-g)),
+ * with w_in[e] = [2 hidden][cols], Wg's rows and then Wu's, and w_out[e] =
+ * [cols][hidden].
+ *   out: y, and zero in rows from the counts on, whose contents nothing reads;
+ *     may be `buffer` itself.
+ *   pre: g and u, for the gradient; rows from the counts on are left as they
+ *     are.
+ * a is rounded to the arrays' type between the two products (16-bit matrix
+ * operands; of the unrounded g and u), and in TACCL_F16 a value of a past 65504
+ * is infinite. Sums run over 32-bit floats; for TACCL_F32 too every product is
+ * one of 32-bit floats. Arrays are contiguous.
+ * 1 <= sources, E <= 1024, 1 <= cols, hidden <= 65536, 1 <= capacity, sources *
+ * capacity <= 2^21, sources * E * capacity < 2^31, and fewer than 2^23 tiles of
+ * 64 rows by 64 columns. cols and hidden in whole 16-byte units and arrays on
+ * 16 bytes are fastest. `workspace`: taccl_ffn_workspace(sources, E, capacity,
+ * hidden, dtype, backward) bytes, 16-byte aligned, not shared with another call
+ * in flight.
+ */
+typedef struct {
+  int64_t capacity;
+  int32_t sources, num_experts, cols, hidden;
+  int32_t dtype; /* of every array but counts */
+  const void *buffer;    /* [sources][E][capacity][cols] */
+  const int32_t *counts; /* [sources][E] */
+  const void *w_in;      /* [E][2 hidden][cols] */
+  const void *w_out;     /* [E][cols][hidden] */
+  void *out;             /* [sources][E][capacity][cols] */
+  void *pre;             /* [sources][E][capacity][2 hidden], or NULL */
+  void *workspace;
+  int64_t workspace_bytes;
+} taccl_ffn_t;
+taccl_status_t taccl_ffn(const taccl_ffn_t *a, taccl_stream_t stream);
+/* 0 for sizes that the calls refuse */
+int64_t taccl_ffn_workspace(int32_t sources, int32_t num_experts, int64_t capacity, int32_t hidden,
+                            int32_t dtype, int32_t backward);
+
+/*
+ * Its gradient for the stored pre: with s = 1 / (1 + exp(-g)) and da = Wo^T dout
+ *   du = da g s, dg = da u s (1 + g (1 - s)), dbuffer = Wg^T dg + Wu^T du,
+ *   dw_in = (dg, du) x^T and dw_out = dout a^T, summed over the rows below the
+ *   counts of all sources.
+ * dbuffer is zero from the counts on, where no input is read; dg, du and a are
+ * rounded to the arrays' type. dbuffer, dw_in, dw_out: each may be NULL, and
+ * none may be another array of the call.
+ */
+typedef struct {
+  int64_t capacity;
+  int32_t sources, num_experts, cols, hidden;
+  int32_t dtype;
+  const void *dout, *buffer;
+  const int32_t *counts;
+  const void *w_in, *w_out, *pre;
+  void *dbuffer, *dw_in, *dw_out;
+  void *workspace;
+  int64_t workspace_bytes;
+} taccl_ffn_backward_t;
+taccl_status_t taccl_ffn_backward(const taccl_ffn_backward_t *a, taccl_stream_t stream);
+
+/*
+ * The whole expert layer of a few tokens, in two launches: the choices and
+ * weights of taccl_route on the logits [tokens][E] (same order, same weights up
+ * to the rounding of 32-bit exponentials), and
+ *   out[t] = sum_j weights[t][j] * Wo_e (silu(Wg_e x[t]) * (Wu_e x[t])),
+ *     e = experts[t][j],
+ * over the choices that lie in first_expert .. first_expert + local_experts - 1,
+ * whose weights w_in and w_out hold: a rank with some of the experts gives its
+ * part, and the ranks' parts add up to the layer. Zero for a token without such
+ * a choice. weights[t][j] * a is held in 32 bits (TACCL_F32) or as the sum of
+ * two numbers of the type (16 bits; past 65504 in TACCL_F16 it is infinite).
+ * experts and weights [tokens][k]: or NULL.
+ * 0 <= tokens <= 64, E <= 1024, k <= min(E, 16), cols, hidden <= 65536.
+ * `workspace`: taccl_ffn_tokens_workspace(tokens, local_experts, k, hidden)
+ * bytes, 16-byte aligned, not shared with another call in flight.
+ */
+typedef struct {
+  int64_t tokens;
+  int32_t cols, hidden;
+  int32_t num_experts, k;
+  int32_t first_expert, local_experts;
+  int32_t dtype;        /* of x, w_in, w_out, out */
+  int32_t logits_dtype; /* of logits */
+  int32_t renorm;
+  const void *x;
+  int64_t x_stride;
+  const void *logits;
+  int64_t logits_stride;
+  const uint8_t *mask; /* [tokens], or NULL */
+  const void *w_in;    /* [local_experts][2 hidden][cols] */
+  const void *w_out;   /* [local_experts][cols][hidden] */
+  void *out;
+  int64_t out_stride;
+  int32_t *experts;
+  float *weights;
+  void *workspace;
+  int64_t workspace_bytes;
+} taccl_ffn_tokens_t;
+taccl_status_t taccl_ffn_tokens(const taccl_ffn_tokens_t *a, taccl_stream_t stream);
+/* 0 for sizes that the call refuses */
+int64_t taccl_ffn_tokens_workspace(int64_t tokens, int32_t local_experts, int32_t k,
+                                   int32_t hidden);
+
+/*
+ * Dropout of rows, with the residual's addition:
+ *   out = residual + (kept ? x / (1 - p) : 0)  (residual NULL: 0),
+ * what is dropped is not looked at. The gradient of x is the same call on the
+ * gradient's rows, with the same rng and without a residual. rng, in device
+ * memory: a seed and an offset. Row r takes the SplitMix64 outputs (see
+ * taccl_generate_host's source) number offset + r * ceil(cols / 2) + 1 and on
+ * of the stream of the seed (modulo 2^64), columns c and c + 1 (c even) the low
+ * and the high 32 bits of one, and a value whose 32 bits are below p * 2^32 is
+ * dropped. A call uses rows * ceil(cols / 2) outputs: add them to the offset for
+ * the next one; a captured call reads rng anew at every replay.
+ * rows <= 2^21, 1 <= cols <= 2^20, 0 <= p <= 1. out may be x or residual, with
+ * the same stride. rows == 0 is a no-op.
+ */
+typedef struct {
+  int64_t rows;
+  int32_t cols;
+  int32_t dtype; /* of x, residual, out */
+  double p;
+  const void *x, *residual;
+  int64_t x_stride, residual_stride;
+  const int64_t *rng; /* [2] */
+  void *out;
+  int64_t out_stride;
+} taccl_dropout_t;
+taccl_status_t taccl_dropout(const taccl_dropout_t *a, taccl_stream_t stream);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char *taccl_last_error(void);
 

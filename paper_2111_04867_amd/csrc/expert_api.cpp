@@ -1,10 +1,12 @@
 // C ABI of the expert-layer operators: checks of arguments and launches.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 #include <string>
 
 #include "expert.h"
+#include "ffn.h"
 #include "plan.h"
 
 namespace taccl {
@@ -64,6 +66,43 @@ void check_buffer(Check &c, const A &a) {
   if (a.tokens == 0) return;
   c.array(a.experts, 4, "experts");
   c.array(a.slots, 4, "slots");
+}
+
+// the sizes that taccl_ffn and its gradient share, and the workspace's
+struct FfnSizes {
+  int64_t sources, experts, capacity, cols, hidden;
+  int32_t dtype;
+};
+void check_ffn_sizes(Check &c, const FfnSizes &z) {
+  c.dtype(z.dtype);
+  c.invalid(z.sources < 1 || z.experts < 1, "sources and num_experts must be at least 1");
+  c.limit(z.sources > kFfnMaxSources, "more than 1024 sources");
+  c.limit(z.experts > kMaxExperts, "more than 1024 experts");
+  c.invalid(z.capacity < 1, "capacity must be at least 1");
+  c.limit(z.capacity > kMaxRows || z.sources * z.capacity > kMaxRows,
+          "more than 2^21 rows of an expert");
+  c.limit(z.sources * z.experts * z.capacity > INT32_MAX, "2^31 rows or more");
+  c.invalid(z.cols < 1 || z.hidden < 1, "cols and hidden must be at least 1");
+  c.limit(z.cols > kFfnMaxCols || z.hidden > kFfnMaxCols, "more than 65536 columns");
+  if (c.st) return;
+  // blocks of the largest grid, whose threads have to stay below 2^32
+  auto tiles = [](int64_t n) { return (n + 63) / 64; };
+  const int64_t rows = tiles(z.sources * z.capacity), wide = tiles(2 * z.hidden);
+  const int64_t most = std::max({rows * wide, rows * tiles(z.cols), tiles(z.cols) * wide});
+  c.limit(z.experts * most >= 1 << 23, "2^23 tiles of 64 x 64 or more");
+}
+template <class A>
+void check_ffn(Check &c, const A &a, bool backward) {
+  const FfnSizes z{a.sources, a.num_experts, a.capacity, a.cols, a.hidden, a.dtype};
+  check_ffn_sizes(c, z);
+  if (c.st) return;
+  const int64_t size = size_of(a.dtype);
+  c.array(a.buffer, size, "buffer");
+  c.array(a.counts, 4, "counts");
+  c.array(a.w_in, size, "w_in");
+  c.array(a.w_out, size, "w_out");
+  c.workspace(a.workspace, a.workspace_bytes,
+              ffn_space(z.sources, z.experts, z.capacity, z.hidden, z.dtype, backward).bytes);
 }
 
 taccl_status_t launched(hipError_t e, const char *call) {
@@ -278,6 +317,112 @@ taccl_status_t taccl_combine_backward(const taccl_combine_backward_t *a, taccl_s
   int cus = 0;
   if (taccl_status_t st = device_cus(c.call, &cus)) return st;
   return launched(launch_combine_backward(*a, cus, (hipStream_t)stream), c.call);
+}
+
+taccl_status_t taccl_ffn(const taccl_ffn_t *a, taccl_stream_t stream) {
+  Check c{"taccl_ffn"};
+  c.invalid(!a, "null arguments");
+  if (c.st) return c.st;
+  check_ffn(c, *a, false);
+  if (c.st) return c.st;
+  c.array(a->out, size_of(a->dtype), "out");
+  c.optional(a->pre, size_of(a->dtype), "pre");
+  if (c.st) return c.st;
+  int cus = 0;
+  if (taccl_status_t st = device_cus(c.call, &cus)) return st;
+  return launched(launch_ffn(*a, cus, (hipStream_t)stream), c.call);
+}
+
+int64_t taccl_ffn_workspace(int32_t sources, int32_t num_experts, int64_t capacity, int32_t hidden,
+                            int32_t dtype, int32_t backward) {
+  Check c{"taccl_ffn_workspace"};
+  check_ffn_sizes(c, FfnSizes{sources, num_experts, capacity, 1, hidden, dtype});
+  return c.st ? 0 : ffn_space(sources, num_experts, capacity, hidden, dtype, backward != 0).bytes;
+}
+
+taccl_status_t taccl_ffn_backward(const taccl_ffn_backward_t *a, taccl_stream_t stream) {
+  Check c{"taccl_ffn_backward"};
+  c.invalid(!a, "null arguments");
+  if (c.st) return c.st;
+  check_ffn(c, *a, true);
+  if (c.st) return c.st;
+  const int64_t size = size_of(a->dtype);
+  c.array(a->dout, size, "dout");
+  c.array(a->pre, size, "pre");
+  c.optional(a->dbuffer, size, "dbuffer");
+  c.optional(a->dw_in, size, "dw_in");
+  c.optional(a->dw_out, size, "dw_out");
+  c.invalid(!a->dbuffer && !a->dw_in && !a->dw_out, "no output");
+  if (c.st) return c.st;
+  int cus = 0;
+  if (taccl_status_t st = device_cus(c.call, &cus)) return st;
+  return launched(launch_ffn_backward(*a, cus, (hipStream_t)stream), c.call);
+}
+
+int64_t taccl_ffn_tokens_workspace(int64_t tokens, int32_t local_experts, int32_t k,
+                                   int32_t hidden) {
+  if (tokens < 0 || tokens > kFfnTokens || local_experts < 1 || local_experts > kMaxExperts ||
+      k < 1 || k > kMaxChoices || hidden < 1 || hidden > kFfnMaxCols)
+    return 0;
+  return ffn_tokens_space(tokens, local_experts, k, hidden);
+}
+
+taccl_status_t taccl_ffn_tokens(const taccl_ffn_tokens_t *a, taccl_stream_t stream) {
+  Check c{"taccl_ffn_tokens"};
+  c.invalid(!a, "null arguments");
+  if (c.st) return c.st;
+  c.invalid(a->tokens < 0, "negative number of tokens");
+  c.limit(a->tokens > kFfnTokens, "more than 64 tokens");
+  c.dtype(a->dtype);
+  c.dtype(a->logits_dtype);
+  c.experts(a->num_experts, a->k);
+  c.invalid(a->k > a->num_experts, "more choices than experts");
+  c.invalid(a->local_experts < 1, "no experts of its own");
+  c.invalid(a->first_expert < 0 ||
+                a->first_expert > (int64_t)a->num_experts - a->local_experts,
+            "the experts of its own are not among the logits'");
+  c.invalid(a->cols < 1 || a->hidden < 1, "cols and hidden must be at least 1");
+  c.limit(a->cols > kFfnMaxCols || a->hidden > kFfnMaxCols, "more than 65536 columns");
+  if (c.st || a->tokens == 0) return c.st;
+  const int64_t size = size_of(a->dtype);
+  c.array(a->x, size, "x");
+  c.stride(a->x_stride, a->cols, a->tokens, "x");
+  c.array(a->logits, size_of(a->logits_dtype), "logits");
+  c.stride(a->logits_stride, a->num_experts, a->tokens, "logits");
+  c.array(a->w_in, size, "w_in");
+  c.array(a->w_out, size, "w_out");
+  c.array(a->out, size, "out");
+  c.stride(a->out_stride, a->cols, a->tokens, "out");
+  c.optional(a->experts, 4, "experts");
+  c.optional(a->weights, 4, "weights");
+  c.workspace(a->workspace, a->workspace_bytes,
+              ffn_tokens_space(a->tokens, a->local_experts, a->k, a->hidden));
+  if (c.st) return c.st;
+  int cus = 0;
+  if (taccl_status_t st = device_cus(c.call, &cus)) return st;
+  return launched(launch_ffn_tokens(*a, cus, (hipStream_t)stream), c.call);
+}
+
+taccl_status_t taccl_dropout(const taccl_dropout_t *a, taccl_stream_t stream) {
+  Check c{"taccl_dropout"};
+  c.invalid(!a, "null arguments");
+  if (c.st) return c.st;
+  c.rows(a->rows);
+  c.dtype(a->dtype);
+  c.invalid(a->cols < 1, "cols must be at least 1");
+  c.limit(a->cols > kDropoutMaxCols, "more than 2^20 columns");
+  c.invalid(!(a->p >= 0 && a->p <= 1), "p must be from 0 to 1");
+  if (c.st || a->rows == 0) return c.st;
+  const int64_t size = size_of(a->dtype);
+  c.array(a->x, size, "x");
+  c.optional(a->residual, size, "residual");
+  c.array(a->rng, 8, "rng");
+  c.array(a->out, size, "out");
+  c.stride(a->x_stride, a->cols, a->rows, "x");
+  if (a->residual) c.stride(a->residual_stride, a->cols, a->rows, "residual");
+  c.stride(a->out_stride, a->cols, a->rows, "out");
+  if (c.st) return c.st;
+  return launched(launch_dropout(*a, (hipStream_t)stream), c.call);
 }
 
 }  // extern "C"

@@ -4,14 +4,17 @@ An Alltoall plan moves chunks of one size between ranks; these operators make
 the chunks and take them back: `norm` gives the token rows (also in 8 bits),
 `route` the experts, places and loads with the loss that keeps them even,
 `dispatch` the send buffer [experts, capacity, dim], whose rows for one rank's
-experts are that rank's chunks (`chunk_bytes` is their size), and `combine`
-the tokens from the rows that come back.
+experts are that rank's chunks (`chunk_bytes` is their size), `ffn` the rows
+through the experts, as they arrive from every rank, and `combine` the tokens
+from the rows that come back; `dropout` adds them to the residual. `ffn_tokens`
+is the whole layer of a few tokens.
 
 `*_tensors` run the library's kernels on the caller's CUDA tensors, on
 `stream` (default: torch's current stream) of the current device, without
 allocating; a tensor made on another stream has to be ready on this one, as
-for any kernel. `norm`, `route`, `dispatch` and `combine` allocate their
-results and are differentiable, once: a second derivative raises. There is no
+for any kernel. `norm`, `route`, `dispatch`, `ffn`, `combine` and `dropout`
+allocate their results and are differentiable, once: a second derivative
+raises. `ffn_tokens` allocates its results and has no gradient. There is no
 fallback: without the library they raise.
 """
 import ctypes as ct
@@ -34,13 +37,14 @@ def _address(name):
 
 _calls.bind(torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
             *(_address(n) for n in ("norm", "norm_backward", "route", "route_backward", "dispatch",
-                                    "combine", "combine_backward")))
+                                    "combine", "combine_backward", "ffn", "ffn_backward",
+                                    "ffn_tokens", "dropout")))
 
 
-def _size(name, arg):
+def _size(name, *args, types=None):
     fn = getattr(binding.lib(), name)
-    fn.argtypes, fn.restype = [ct.c_int32], ct.c_int64
-    return fn(arg)
+    fn.argtypes, fn.restype = types or [ct.c_int32] * len(args), ct.c_int64
+    return fn(*args)
 
 
 def norm_workspace(cols):
@@ -51,6 +55,39 @@ def norm_workspace(cols):
 def route_workspace(num_experts):
     """Bytes of route_tensors' workspace."""
     return _size("taccl_route_workspace", int(num_experts))
+
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _fits(*sizes):
+    return all(0 <= n < 1 << 31 for n in sizes)
+
+
+def ffn_workspace(shape, hidden, dtype, backward=False):
+    """Bytes of ffn_tensors' workspace (backward: ffn_backward_tensors') for
+    rows of `shape` [experts, capacity, dim] or [sources, experts, capacity,
+    dim]; 0 for sizes that they refuse."""
+    s, e, c = (1, *shape[:2]) if len(shape) == 3 else shape[:3]
+    if not _fits(s, e, c, hidden):
+        return 0
+    return _size("taccl_ffn_workspace", s, e, c, hidden, _DTYPES.get(dtype, -1), int(backward),
+                 types=[ct.c_int32, ct.c_int32, ct.c_int64] + [ct.c_int32] * 3)
+
+
+def ffn_tokens_workspace(tokens, num_experts, k, hidden):
+    """Bytes of ffn_tokens_tensors' workspace; num_experts are those that its
+    weights hold. 0 for sizes that it refuses."""
+    if not _fits(tokens, num_experts, k, hidden):
+        return 0
+    return _size("taccl_ffn_tokens_workspace", tokens, num_experts, k, hidden,
+                 types=[ct.c_int64] + [ct.c_int32] * 3)
+
+
+def dropout_words(rows, cols):
+    """Random numbers that a call of dropout uses: what to add to rng[1]
+    before the next one."""
+    return rows * ((cols + 1) // 2)
 
 
 def chunk_bytes(num_experts, capacity, row_bytes, ranks, chunks_per_pair=1):
@@ -136,6 +173,48 @@ def combine_backward_tensors(dout, buffer, experts, slots, counts, weights, dbuf
     """taccl_combine_backward: dbuffer (zero from counts on) and dweights."""
     st = _calls.combine_backward(dout, buffer, experts, slots, counts, weights, dbuffer, dweights,
                                  stream and stream.cuda_stream)
+    if st:
+        binding._check(st)
+
+
+def ffn_tensors(buffer, counts, w_in, w_out, out, workspace, *, pre=None, stream=None):
+    """taccl_ffn: out = w_out[e] (silu(g) * u) with (g, u) = w_in[e] x for the
+    rows x of buffer [experts, capacity, dim] or [sources, experts, capacity,
+    dim] below counts int32 [experts] or [sources, experts], zero from there
+    on; w_in [experts, 2 hidden, dim], w_out [experts, dim, hidden]. pre [...,
+    2 hidden] keeps g and u for the gradient. out may be buffer."""
+    st = _calls.ffn(buffer, counts, w_in, w_out, out, workspace, pre,
+                    stream and stream.cuda_stream)
+    if st:
+        binding._check(st)
+
+
+def ffn_backward_tensors(dout, buffer, counts, w_in, w_out, pre, workspace, *, dbuffer=None,
+                         dw_in=None, dw_out=None, stream=None):
+    """taccl_ffn_backward: the gradients that are given, dbuffer (zero from
+    counts on), dw_in and dw_out."""
+    st = _calls.ffn_backward(dout, buffer, counts, w_in, w_out, pre, workspace, dbuffer, dw_in,
+                             dw_out, stream and stream.cuda_stream)
+    if st:
+        binding._check(st)
+
+
+def ffn_tokens_tensors(x, logits, w_in, w_out, out, workspace, *, k, mask=None, renorm=True,
+                       first_expert=0, experts=None, weights=None, stream=None):
+    """taccl_ffn_tokens: route's choices of up to 64 tokens x [tokens, dim] by
+    logits [tokens, experts] and, in out, the weighted sum over them of ffn
+    with the weights w_in and w_out of the experts from first_expert on; the
+    choices go to experts int32 and weights float32 [tokens, k]."""
+    st = _calls.ffn_tokens(x, logits, w_in, w_out, out, workspace, k, mask, renorm, first_expert,
+                           experts, weights, stream and stream.cuda_stream)
+    if st:
+        binding._check(st)
+
+
+def dropout_tensors(x, rng, out, *, p, residual=None, stream=None):
+    """taccl_dropout: out = residual + (kept ? x / (1 - p) : 0), by the random
+    numbers of rng int64 [2] (seed and offset, on the device)."""
+    st = _calls.dropout(x, rng, out, p, residual, stream and stream.cuda_stream)
     if st:
         binding._check(st)
 
@@ -278,3 +357,87 @@ def combine(buffer, experts, slots, counts, weights):
     """Tokens [tokens, dim] of combine_tensors; gradients flow to the buffer
     and the weights (None: 1)."""
     return _CombineFn.apply(buffer, experts, slots, counts, weights)
+
+
+class _FfnFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, buffer, counts, w_in, w_out):
+        hidden = w_out.shape[2]
+        out = torch.empty_like(buffer)
+        pre = None
+        if any(ctx.needs_input_grad):
+            pre = torch.empty(*buffer.shape[:-1], 2 * hidden, dtype=buffer.dtype,
+                              device=buffer.device)
+        ffn_tensors(buffer, counts, w_in, w_out, out,
+                    _workspace(ffn_workspace(buffer.shape, hidden, buffer.dtype), buffer), pre=pre)
+        ctx.save_for_backward(buffer, counts, w_in, w_out, pre)
+        return out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout):
+        buffer, counts, w_in, w_out, pre = ctx.saved_tensors
+        want = ctx.needs_input_grad
+        given = [torch.empty_like(t) if need else None
+                 for t, need in ((buffer, want[0]), (w_in, want[2]), (w_out, want[3]))]
+        size = ffn_workspace(buffer.shape, w_out.shape[2], buffer.dtype, True)
+        ffn_backward_tensors(dout.contiguous(), buffer, counts, w_in, w_out, pre,
+                             _workspace(size, buffer), dbuffer=given[0], dw_in=given[1],
+                             dw_out=given[2])
+        return given[0], None, given[1], given[2]
+
+
+def ffn(buffer, counts, w_in, w_out):
+    """Rows of ffn_tensors; gradients flow to the buffer and the weights."""
+    return _FfnFn.apply(buffer, counts, w_in, w_out)
+
+
+class _FfnTokensFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, logits, k, w_in, w_out, mask, renorm, first_expert):
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        experts = torch.empty(len(x), k, dtype=torch.int32, device=x.device)
+        weights = torch.empty(len(x), k, device=x.device)
+        size = ffn_tokens_workspace(len(x), len(w_out), k, w_out.shape[2])
+        ffn_tokens_tensors(x, logits, w_in, w_out, out, _workspace(size, x), k=k, mask=mask,
+                           renorm=renorm, first_expert=first_expert, experts=experts,
+                           weights=weights)
+        ctx.mark_non_differentiable(experts)
+        return out, experts, weights
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("ffn_tokens has no gradient: take route, dispatch, ffn and combine")
+
+
+def ffn_tokens(x, logits, k, w_in, w_out, *, mask=None, renorm=True, first_expert=0):
+    """(out, experts, weights) of ffn_tokens_tensors, without a gradient."""
+    return _FfnTokensFn.apply(x, logits, k, w_in, w_out, mask, renorm, first_expert)
+
+
+class _DropoutFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, rng, p, residual):
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        dropout_tensors(x, rng, out, p=p, residual=residual)
+        ctx.save_for_backward(rng)
+        ctx.p = p
+        return out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout):
+        rng, = ctx.saved_tensors
+        dx = None
+        if ctx.needs_input_grad[0]:
+            dx = torch.empty(dout.shape, dtype=dout.dtype, device=dout.device)
+            dropout_tensors(_gradient_rows(dout), rng, dx, p=ctx.p)
+        return dx, None, None, dout if ctx.needs_input_grad[3] else None
+
+
+def dropout(x, p, rng, residual=None):
+    """Rows of dropout_tensors; gradients flow to x and the residual. The
+    gradient draws the same numbers again, so rng has to stay as it is until
+    then (a changed one raises): give every call its own, `rng + offset`, or
+    step a shared one between the training steps."""
+    return _DropoutFn.apply(x, rng, p, residual)

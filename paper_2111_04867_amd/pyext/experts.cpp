@@ -35,6 +35,10 @@ Fn<taccl_route_backward_t> route_backward_fn;
 Fn<taccl_dispatch_t> dispatch_fn;
 Fn<taccl_combine_t> combine_fn;
 Fn<taccl_combine_backward_t> combine_backward_fn;
+Fn<taccl_ffn_t> ffn_fn;
+Fn<taccl_ffn_backward_t> ffn_backward_fn;
+Fn<taccl_ffn_tokens_t> ffn_tokens_fn;
+Fn<taccl_dropout_t> dropout_fn;
 
 // a Python error that is set already
 struct Raised {};
@@ -349,6 +353,115 @@ PyObject *combine_backward(PyObject *const *o) {
   return run(combine_backward_fn, a, at);
 }
 
+// Sizes of the experts' feed-forward by its rows [sources, experts, capacity,
+// dim] (or without sources) and w_out [experts, dim, hidden], and the arrays
+// that both passes have.
+template <class A>
+void ffn_arrays(A &a, const At &at, const Tensor &b, PyObject *counts, PyObject *w_in,
+                PyObject *w_out, PyObject *workspace) {
+  const int64_t s = b.dim() == 4 ? b.size(0) : 1, e = b.size(-3), d = b.size(-1);
+  const Tensor &w = tensor(w_out, "w_out");
+  if (w.dim() != 3) misfit(w, "w_out", "a tensor [experts, dim, hidden]");
+  const int64_t f = w.size(2);
+  a.sources = size32(s);
+  a.num_experts = size32(e);
+  a.capacity = b.size(-2);
+  a.cols = size32(d);
+  a.hidden = size32(f);
+  a.buffer = b.data_ptr();
+  if (b.dim() == 4) at.flat(counts, "counts", {s, e}, at::kInt, a.counts);
+  else at.flat(counts, "counts", {e}, at::kInt, a.counts);
+  at.flat(w_in, "w_in", {e, 2 * f, d}, b.scalar_type(), a.w_in);
+  at.flat(w_out, "w_out", {e, d, f}, b.scalar_type(), a.w_out);
+  at.workspace(workspace, a.workspace, a.workspace_bytes);
+}
+const Tensor &ffn_buffer(PyObject *o, const char *name) {
+  const Tensor &t = tensor(o, name);
+  if ((t.dim() != 3 && t.dim() != 4) || !t.is_contiguous() || t.get_device() < 0)
+    misfit(t, name, "a contiguous CUDA tensor [experts, capacity, dim] or with sources before");
+  return t;
+}
+// rows of `cols` columns where `b` has rows
+template <class P>
+void ffn_rows(const At &at, PyObject *o, const char *name, const Tensor &b, int64_t cols, P *&p) {
+  if (b.dim() == 4) at.flat(o, name, {b.size(0), b.size(1), b.size(2), cols}, b.scalar_type(), p);
+  else at.flat(o, name, {b.size(0), b.size(1), cols}, b.scalar_type(), p);
+}
+
+// buffer, counts, w_in, w_out, out, workspace, pre, stream
+PyObject *ffn(PyObject *const *o) {
+  const Tensor &b = ffn_buffer(o[0], "buffer");
+  taccl_ffn_t a{};
+  a.dtype = dtype_code(b, "buffer", false);
+  const At at(b, "buffer", o[7]);
+  ffn_arrays(a, at, b, o[1], o[2], o[3], o[5]);
+  ffn_rows(at, o[4], "out", b, b.size(-1), a.out);
+  ffn_rows(at, o[6], "pre", b, 2 * (int64_t)a.hidden, a.pre);
+  return run(ffn_fn, a, at);
+}
+
+// dout, buffer, counts, w_in, w_out, pre, workspace, dbuffer, dw_in, dw_out, stream
+PyObject *ffn_backward(PyObject *const *o) {
+  const Tensor &b = ffn_buffer(o[1], "buffer");
+  taccl_ffn_backward_t a{};
+  a.dtype = dtype_code(b, "buffer", false);
+  const At at(b, "buffer", o[10]);
+  ffn_arrays(a, at, b, o[2], o[3], o[4], o[6]);
+  const int64_t e = b.size(-3), d = b.size(-1), f = a.hidden;
+  ffn_rows(at, o[0], "dout", b, d, a.dout);
+  ffn_rows(at, o[5], "pre", b, 2 * f, a.pre);
+  ffn_rows(at, o[7], "dbuffer", b, d, a.dbuffer);
+  at.flat(o[8], "dw_in", {e, 2 * f, d}, b.scalar_type(), a.dw_in);
+  at.flat(o[9], "dw_out", {e, d, f}, b.scalar_type(), a.dw_out);
+  return run(ffn_backward_fn, a, at);
+}
+
+// x, logits, w_in, w_out, out, workspace, k, mask, renorm, first_expert, experts, weights, stream
+PyObject *ffn_tokens(PyObject *const *o) {
+  const Tensor &x = tensor(o[0], "x"), &l = tensor(o[1], "logits"), &w = tensor(o[3], "w_out");
+  taccl_ffn_tokens_t a{};
+  a.dtype = dtype_code(x, "x", true);
+  a.logits_dtype = dtype_code(l, "logits", true);
+  const ScalarType type = x.scalar_type();
+  const At at(x, "x", o[12]);
+  if (w.dim() != 3) misfit(w, "w_out", "a tensor [experts, dim, hidden]");
+  const int64_t n = a.tokens = x.size(0), d = x.size(1), own = w.size(0), f = w.size(2);
+  a.cols = size32(d);
+  a.hidden = size32(f);
+  a.num_experts = size32(l.size(1));
+  a.local_experts = size32(own);
+  a.k = small(o[6], "k");
+  a.renorm = PyObject_IsTrue(o[8]);
+  a.first_expert = small(o[9], "first_expert");
+  at.rows(x, "x", n, d, type, a.x, a.x_stride);
+  at.rows(l, "logits", n, l.size(1), l.scalar_type(), a.logits, a.logits_stride);
+  at.mask(o[7], n, a.mask);
+  at.flat(o[2], "w_in", {own, 2 * f, d}, type, a.w_in);
+  at.flat(o[3], "w_out", {own, d, f}, type, a.w_out);
+  at.rows(o[4], "out", n, d, type, a.out, a.out_stride);
+  at.flat(o[10], "experts", {n, a.k}, at::kInt, a.experts);
+  at.flat(o[11], "weights", {n, a.k}, at::kFloat, a.weights);
+  at.workspace(o[5], a.workspace, a.workspace_bytes);
+  return run(ffn_tokens_fn, a, at);
+}
+
+// x, rng, out, p, residual, stream
+PyObject *dropout(PyObject *const *o) {
+  const Tensor &x = tensor(o[0], "x");
+  taccl_dropout_t a{};
+  a.dtype = dtype_code(x, "x", true);
+  const ScalarType type = x.scalar_type();
+  const At at(x, "x", o[5]);
+  const int64_t n = a.rows = x.size(0), d = x.size(1);
+  a.cols = size32(d);
+  a.p = real(o[3]);
+  at.rows(x, "x", n, d, type, a.x, a.x_stride);
+  at.rows(o[4], "residual", n, d, type, a.residual, a.residual_stride);
+  at.flat(o[1], "rng", {2}, at::kLong, a.rng);
+  at.rows(o[2], "out", n, d, type, a.out, a.out_stride);
+  return run(dropout_fn, a, at);
+}
+
 template <PyObject *(*kCall)(PyObject *const *), int kArgs>
 PyObject *checked(PyObject *, PyObject *const *o, Py_ssize_t n) {
   if (n != kArgs) {
@@ -369,9 +482,9 @@ PyObject *checked(PyObject *, PyObject *const *o, Py_ssize_t n) {
 // bind(current device, current stream, addresses of the library's calls)
 PyObject *bind(PyObject *, PyObject *args) {
   PyObject *device, *stream;
-  unsigned long long f[7];
-  if (!PyArg_ParseTuple(args, "OOKKKKKKK", &device, &stream, f, f + 1, f + 2, f + 3, f + 4, f + 5,
-                        f + 6))
+  unsigned long long f[11];
+  if (!PyArg_ParseTuple(args, "OOKKKKKKKKKKK", &device, &stream, f, f + 1, f + 2, f + 3, f + 4,
+                        f + 5, f + 6, f + 7, f + 8, f + 9, f + 10))
     return nullptr;
   Py_INCREF(device);
   Py_INCREF(stream);
@@ -386,6 +499,10 @@ PyObject *bind(PyObject *, PyObject *args) {
   dispatch_fn = (Fn<taccl_dispatch_t>)f[4];
   combine_fn = (Fn<taccl_combine_t>)f[5];
   combine_backward_fn = (Fn<taccl_combine_backward_t>)f[6];
+  ffn_fn = (Fn<taccl_ffn_t>)f[7];
+  ffn_backward_fn = (Fn<taccl_ffn_backward_t>)f[8];
+  ffn_tokens_fn = (Fn<taccl_ffn_tokens_t>)f[9];
+  dropout_fn = (Fn<taccl_dropout_t>)f[10];
   Py_RETURN_NONE;
 }
 
@@ -399,6 +516,10 @@ PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                          CALL(dispatch, 8),
                          CALL(combine, 6),
                          CALL(combine_backward, 9),
+                         CALL(ffn, 8),
+                         CALL(ffn_backward, 11),
+                         CALL(ffn_tokens, 13),
+                         CALL(dropout, 6),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_experts", nullptr, -1, methods,
                       nullptr,               nullptr,    nullptr, nullptr};

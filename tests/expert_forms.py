@@ -180,3 +180,143 @@ def combine_backward(dout, buffer, experts, slots, weights):
         dw[t, j] = (d[t] * b[e, s]).sum()
         size[t, j] = (d[t] * b[e, s]).abs().sum()
     return db, dw, size
+
+
+# ---- the experts' feed-forward -------------------------------------------------------
+# Errors are to first order, with every sum of n products in 32 bits off by at
+# most n U of the products' sizes, in whatever order it is taken, and a sigmoid
+# by (|g| + 12) U of itself: the exponent's product is rounded, |g| U, then the
+# exponential and the reciprocal are within two units in the last place each and
+# two more operations are rounded.
+
+def held(counts, capacity):
+    """Rows of every (source, expert) [S, E]."""
+    return counts.cpu().clamp(0, capacity).long()
+
+
+def _stored(v, dtype):
+    """What rounding v to a stored type may add."""
+    rel, step = ROUND[dtype]
+    return rel * v.abs() + step
+
+
+def _sigmoid_slack(g):
+    return (g.abs() + 12) * U
+
+
+def _gated(x, w_in, w_out, dtype, halves=1, weight=None):
+    """One expert's rows in 64 bits: (y, slack of y, (g, u), slack of (g, u)).
+    `a` is stored as the sum of `halves` numbers of the type."""
+    f = w_out.shape[1]
+    pre = x @ w_in.T
+    pre_slack = x.shape[1] * U * (x.abs() @ w_in.abs().T)
+    (g, u), (dg, du) = pre.split(f, 1), pre_slack.split(f, 1)
+    s = torch.sigmoid(g)
+    a = g * s * u
+    da = 1.1 * dg * u.abs() + (g * s).abs() * du + a.abs() * (_sigmoid_slack(g) + 3 * U)
+    if weight is not None:
+        a, da = a * weight[0], da * weight[0] + a.abs() * weight[1]
+    rel, step = ROUND[dtype]
+    da = da + rel ** halves * a.abs() + step
+    y = a @ w_out.T
+    slack = da @ w_out.abs().T + f * U * (a.abs() @ w_out.abs().T)
+    return y, 1.01 * slack, pre, pre_slack
+
+
+def ffn(buffer, counts, w_in, w_out):
+    """(out, its slack, pre, its slack), zero from the counts on."""
+    dtype, (s, e, c, d) = buffer.dtype, buffer.shape
+    f = w_out.shape[2]
+    n = held(counts, c)
+    out, slack = (torch.zeros(s, e, c, d, dtype=torch.float64) for _ in range(2))
+    pre, pre_slack = (torch.zeros(s, e, c, 2 * f, dtype=torch.float64) for _ in range(2))
+    x, wi, wo = (t.cpu().double() for t in (buffer, w_in, w_out))
+    for j in range(e):
+        for i in range(s):
+            r = (i, j, slice(0, int(n[i, j])))
+            out[r], slack[r], pre[r], pre_slack[r] = _gated(x[r], wi[j], wo[j], dtype)
+    return out, slack, pre, pre_slack
+
+
+def ffn_backward(dout, buffer, counts, w_in, w_out, pre):
+    """((dbuffer, slack), (dw_in, slack), (dw_out, slack))."""
+    dtype, (s, e, c, d) = buffer.dtype, buffer.shape
+    n = held(counts, c)
+    dy, x, wi, wo, h = (t.cpu().double() for t in (dout, buffer, w_in, w_out, pre))
+    db, dbs = torch.zeros_like(x), torch.zeros_like(x)
+    dwi, dwis, dwo, dwos = (torch.zeros_like(t) for t in (wi, wi, wo, wo))
+    for j in range(e):
+        at = [(i, j, slice(0, int(n[i, j]))) for i in range(s)]
+        rows = sum(int(n[i, j]) for i in range(s))
+        for r in at:
+            g, u = h[r].chunk(2, 1)
+            sg = torch.sigmoid(g)
+            eps = _sigmoid_slack(g)
+            slope = sg * (1 + g * (1 - sg))
+            da = dy[r] @ wo[j]
+            das = d * U * (dy[r].abs() @ wo[j].abs())
+            a = g * sg * u
+            a_s = a.abs() * (eps + 3 * U) + _stored(a, dtype)
+            du = da * g * sg
+            dus = (g * sg).abs() * das + du.abs() * (eps + 3 * U) + _stored(du, dtype)
+            dg = da * u * slope
+            dgs = ((u * slope).abs() * das + (da * u).abs() * 3 * eps * sg * (1 + g.abs())
+                   + 4 * U * dg.abs() + _stored(dg, dtype))
+            dp, dps = torch.cat([dg, du], 1), torch.cat([dgs, dus], 1)
+            db[r] = dp @ wi[j]
+            dbs[r] = 1.01 * (dps @ wi[j].abs() + dp.shape[1] * U * (dp.abs() @ wi[j].abs()))
+            dwi[j] += dp.T @ x[r]
+            dwis[j] += 1.01 * (dps.T @ x[r].abs() + rows * U * (dp.abs().T @ x[r].abs()))
+            dwo[j] += dy[r].T @ a
+            dwos[j] += 1.01 * (dy[r].abs().T @ a_s + rows * U * (dy[r].abs().T @ a.abs()))
+    return (db, dbs), (dwi, dwis), (dwo, dwos)
+
+
+def ffn_tokens(x, logits, k, w_in, w_out, mask=None, renorm=True, first=0):
+    """(out, its slack, experts, weights, their slack). A weight is a quotient of
+    32-bit exponentials, each off by its exponent's rounding (the row's spread)
+    and a few units, and of a sum of up to E of them."""
+    r = route(logits, k, mask, 0, 0.0, renorm)
+    rel = (2 * logit_range(logits, mask) + logits.shape[1] + 20) * U
+    xs, wi, wo = (t.cpu().double() for t in (x, w_in, w_out))
+    out = torch.zeros(len(xs), wo.shape[1], dtype=torch.float64)
+    slack = out.clone()
+    halves = 1 if x.dtype == torch.float32 else 2
+    for t, chosen in enumerate(r["experts"].tolist()):
+        for j, e in enumerate(chosen):
+            if e >= 0 and 0 <= e - first < len(wo):
+                w = r["weights"][t, j]
+                y, s, _, _ = _gated(xs[t:t + 1], wi[e - first], wo[e - first], x.dtype, halves,
+                                    (w, w * rel + 1e-38))
+                out[t] += y[0]
+                slack[t] += s[0]
+    return out, slack + k * U * out.abs(), r["experts"], r["weights"], r["weights"] * rel + 1e-38
+
+
+# ---- dropout ----------------------------------------------------------------------
+
+def kept(rng, rows, cols, p):
+    """Truth values [rows, cols], one word after the other."""
+    seed, offset = (int(v) % 2 ** 64 for v in rng.tolist())
+    half, below, full = (cols + 1) // 2, p * 2 ** 32, 2 ** 64 - 1
+    out = torch.empty(rows, 2 * half, dtype=torch.bool)
+    for i in range(rows * half):
+        z = (seed + (offset + i + 1) * 0x9E3779B97F4A7C15) & full
+        z = (z ^ z >> 30) * 0xBF58476D1CE4E5B9 & full
+        z = (z ^ z >> 27) * 0x94D049BB133111EB & full
+        z ^= z >> 31
+        out[i // half, i % half * 2] = (z & 0xFFFFFFFF) >= below
+        out[i // half, i % half * 2 + 1] = (z >> 32) >= below
+    return out[:, :cols]
+
+
+def dropout(x, rng, p, residual=None):
+    """(out, slack): the scale, its product and the sum are rounded once each."""
+    y = torch.zeros(x.shape, dtype=torch.float64)
+    keep = kept(rng, *x.shape, p)
+    y[keep] = x.cpu().double()[keep] / (1 - p)
+    slack = 2.1 * U * y.abs()
+    if residual is not None:
+        y = y + residual.cpu().double()
+        slack = slack + U * y.abs()
+    return y, slack

@@ -1,0 +1,114 @@
+"""The expert layer of a few tokens against the 64-bit form and the router."""
+import pytest
+import torch
+
+import expert_forms as F
+from paper_2111_04867_amd import experts as X
+
+pytestmark = pytest.mark.gpu
+TYPES = pytest.mark.parametrize("dtype", F.TYPES.values(), ids=F.TYPES)
+
+# tokens, experts, k, dim, hidden
+CASES = [(1, 1, 1, 1, 1), (1, 8, 2, 64, 16), (2, 4, 4, 40, 24), (16, 16, 2, 72, 48),
+         (17, 9, 3, 111, 77), (33, 70, 8, 130, 33), (64, 300, 16, 64, 32), (5, 1024, 4, 24, 8),
+         (3, 4, 2, 1111, 515), (32, 12, 5, 520, 264), (64, 3, 3, 2056, 72)]
+
+
+def make(dtype, t, e, k, d, f, seed=0, pad=0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+
+    def randn(*shape):
+        return torch.randn(*shape, generator=gen, device="cuda")
+
+    return {"x": randn(t, d + pad).to(dtype)[:, :d], "logits": 2 * randn(t, e + pad)[:, :e],
+            "w_in": (randn(e, 2 * f, d) / d ** 0.5).to(dtype),
+            "w_out": (randn(e, d, f) / f ** 0.5).to(dtype)}
+
+
+def run(m, k, **options):
+    t, d = m["x"].shape
+    out = torch.full((t, d + 3), 7.0, dtype=m["x"].dtype, device="cuda")
+    experts = torch.full((t, k), -9, dtype=torch.int32, device="cuda")
+    weights = torch.full((t, k), float("nan"), device="cuda")
+    n = X.ffn_tokens_workspace(t, len(m["w_out"]), k, m["w_out"].shape[2])
+    work = torch.full((n + 256,), 0xFF, dtype=torch.uint8, device="cuda")  # NaN in every type
+    X.ffn_tokens_tensors(m["x"], m["logits"], m["w_in"], m["w_out"], out[:, :d], work[:n], k=k,
+                         experts=experts, weights=weights, **options)
+    assert (out[:, d:] == 7).all() and (work[n:] == 0xFF).all()
+    return out[:, :d], experts, weights
+
+
+def check(m, k, dtype, **options):
+    got = run(m, k, **options)
+    form = {("first" if n == "first_expert" else n): v for n, v in options.items()}
+    out, slack, experts, weights, weight_slack = F.ffn_tokens(m["x"], m["logits"], k, m["w_in"],
+                                                              m["w_out"], **form)
+    assert torch.equal(got[1].cpu(), experts)
+    F.close(got[2], weights, torch.float32, weight_slack)
+    F.close(got[0], out, dtype, slack)
+    return got
+
+
+@TYPES
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_tokens(dtype, case):
+    check(make(dtype, *case), case[2], dtype)
+
+
+@TYPES
+@pytest.mark.parametrize("case", CASES[3:6], ids=str)
+def test_masks_strides_and_plain_weights(dtype, case):
+    m = make(dtype, *case, seed=1, pad=5)
+    mask = (torch.arange(case[0], device="cuda") % 3 != 1).to(torch.uint8)
+    m["x"][1] = float("nan")
+    m["logits"][1] = float("nan")
+    check(m, case[2], dtype, mask=mask, renorm=False)
+    check(m, case[2], dtype, mask=mask.bool(), renorm=True)
+
+
+@TYPES
+def test_a_part_of_the_experts(dtype):
+    """The parts of the ranks add up to the layer."""
+    m = make(dtype, 20, 12, 3, 64, 40, seed=2)
+    whole = check(m, 3, dtype)[0].double()
+    parts = 0
+    for first in (0, 5, 6):
+        n = {0: 5, 5: 1, 6: 6}[first]
+        own = dict(m, w_in=m["w_in"][first:first + n], w_out=m["w_out"][first:first + n])
+        parts = parts + check(own, 3, dtype, first_expert=first)[0].double()
+    rel = F.ROUND[dtype][0]
+    # four roundings of numbers of about the output's size
+    assert (parts - whole).abs().max() <= 8 * rel * whole.abs().max()
+
+
+def test_the_routers_choices():
+    """Ties, both zeros, infinities and NaN: as route chooses."""
+    m = make(torch.float32, 40, 24, 4, 16, 8, seed=3)
+    x = m["logits"]
+    x[0] = 0
+    x[1] = 0
+    x[1, ::2] = -0.0
+    x[2] = float("-inf")
+    x[3] = float("-inf")
+    x[3, 5] = 1.0
+    x[4, 7] = float("nan")
+    x[5] = torch.finfo(torch.float32).min
+    x[6] = (x[6] * 2).round() / 2
+    x[7, 3] = float("inf")
+    x[8] = -1e30
+    x[9] = 1e9 + 64 * x[9].round()
+    for renorm in (True, False):
+        out, experts, weights = run(m, 4, renorm=renorm)
+        want = X.route(x, 4, renorm=renorm)
+        assert torch.equal(experts, want[0])
+        assert torch.allclose(weights, want[1], rtol=1e-5, atol=1e-37, equal_nan=True)
+        assert (out[2] == 0).all()
+        fine = want[1].isfinite().all(1)
+        assert out[fine].isfinite().all() and int(fine.sum()) >= 38
+
+
+@pytest.mark.parametrize("logits", F.TYPES.values(), ids=F.TYPES)
+def test_types_of_logits(logits):
+    m = make(torch.bfloat16, 9, 30, 4, 64, 32, seed=4)
+    m["logits"] = m["logits"].to(logits)
+    check(m, 4, torch.bfloat16)
