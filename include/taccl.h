@@ -631,8 +631,7 @@ taccl_status_t taccl_ffn_backward(const taccl_ffn_backward_t *a, taccl_stream_t 
  * two numbers of the type (16 bits; past 65504 in TACCL_F16 it is infinite).
  * experts and weights [tokens][k]: or NULL.
  * 0 <= tokens <= 64, E <= 1024, k <= min(E, 16), cols, hidden <= 65536.
- * `workspace`: taccl_ffn_tokens_workspace(tokens, local_experts, k, hidden)
- * bytes, 16-byte aligned, not shared with another call in flight.
+ * `workspace`: taccl_ffn_tokens_workspace(tokens, k, cols, hidden) bytes, 16-byte aligned, not shared with another call in flight.
  */
 typedef struct {
   int64_t tokens;
@@ -658,8 +657,7 @@ typedef struct {
 } taccl_ffn_tokens_t;
 taccl_status_t taccl_ffn_tokens(const taccl_ffn_tokens_t *a, taccl_stream_t stream);
 /* 0 for sizes that the call refuses */
-int64_t taccl_ffn_tokens_workspace(int64_t tokens, int32_t local_experts, int32_t k,
-                                   int32_t hidden);
+int64_t taccl_ffn_tokens_workspace(int64_t tokens, int32_t k, int32_t cols, int32_t hidden);
 
 /*
  * Dropout of rows, with the residual's addition:

@@ -359,12 +359,11 @@ taccl_status_t taccl_ffn_backward(const taccl_ffn_backward_t *a, taccl_stream_t 
   return launched(launch_ffn_backward(*a, cus, (hipStream_t)stream), c.call);
 }
 
-int64_t taccl_ffn_tokens_workspace(int64_t tokens, int32_t local_experts, int32_t k,
-                                   int32_t hidden) {
-  if (tokens < 0 || tokens > kFfnTokens || local_experts < 1 || local_experts > kMaxExperts ||
-      k < 1 || k > kMaxChoices || hidden < 1 || hidden > kFfnMaxCols)
+int64_t taccl_ffn_tokens_workspace(int64_t tokens, int32_t k, int32_t cols, int32_t hidden) {
+  if (tokens < 0 || tokens > kFfnTokens || k < 1 || k > kMaxChoices || cols < 1 ||
+      cols > kFfnMaxCols || hidden < 1 || hidden > kFfnMaxCols)
     return 0;
-  return ffn_tokens_space(tokens, local_experts, k, hidden);
+  return ffn_tokens_space(tokens, k, cols, hidden);
 }
 
 taccl_status_t taccl_ffn_tokens(const taccl_ffn_tokens_t *a, taccl_stream_t stream) {
@@ -396,7 +395,7 @@ taccl_status_t taccl_ffn_tokens(const taccl_ffn_tokens_t *a, taccl_stream_t stre
   c.optional(a->experts, 4, "experts");
   c.optional(a->weights, 4, "weights");
   c.workspace(a->workspace, a->workspace_bytes,
-              ffn_tokens_space(a->tokens, a->local_experts, a->k, a->hidden));
+              ffn_tokens_space(a->tokens, a->k, a->cols, a->hidden));
   if (c.st) return c.st;
   int cus = 0;
   if (taccl_status_t st = device_cus(c.call, &cus)) return st;

@@ -33,7 +33,7 @@ FfnSpace ffn_space(int64_t sources, int64_t experts, int64_t capacity, int64_t h
 // Arguments are the C ABI's, checked.
 hipError_t launch_ffn(const taccl_ffn_t &a, int cus, hipStream_t stream);
 hipError_t launch_ffn_backward(const taccl_ffn_backward_t &a, int cus, hipStream_t stream);
-int64_t ffn_tokens_space(int64_t tokens, int64_t experts, int64_t k, int64_t hidden);
+int64_t ffn_tokens_space(int64_t tokens, int64_t k, int64_t cols, int64_t hidden);
 hipError_t launch_ffn_tokens(const taccl_ffn_tokens_t &a, int cus, hipStream_t stream);
 hipError_t launch_dropout(const taccl_dropout_t &a, hipStream_t stream);
 

@@ -22,16 +22,27 @@ namespace taccl {
 namespace {
 
 constexpr int kTokens = kFfnTokens;
-constexpr int kUpWaves = 8, kDownWaves = 16;
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+// blocks that a CU holds
+constexpr int kPerCu = 4;
+template <class T>
+constexpr int kDownPerCu = sizeof(T) == 4 ? 4 : 3;
+constexpr int kMaxParts = 16;
 
-// The workspace: the chosen experts, then w a of every (expert, token) in
-// chunks along the hidden axis: 4 floats, or 8 values as the sum of two 16-bit
-// numbers (the weights are 16-bit then; a rounded to 16 bits would be off by as
-// much as the result's own rounding, and the second product costs nothing that
-// the weights' reading does not hide).
+// An entry is up to 16 tokens that chose the same expert: the columns of one
+// matrix operand.
+constexpr int kMaxEntries = kTokens * kMaxChoices;
+
+// The workspace: the entries, then w a of every one of their tokens: a row of
+// floats, or two of 16-bit numbers whose sum it is (the weights are 16-bit then;
+// a rounded to 16 bits would be off by as much as the result's own rounding, and
+// the second product costs nothing that the weights' reading does not hide).
 struct Chosen {
   int32_t n;
-  int32_t experts[kMaxExperts];
+  uint32_t tokens[kMaxEntries][2];  // bits
+  int16_t experts[kMaxEntries];
+  int16_t rows[kMaxEntries];  // the first token's row
+  int32_t done[kFfnMaxCols / 16];  // parts of a tile of columns that are there
 };
 constexpr int64_t kChosenBytes = (sizeof(Chosen) + 255) / 256 * 256;
 
@@ -41,180 +52,279 @@ struct TokensArgs {
   taccl_ffn_tokens_t a;
   Chosen *chosen;
   uint8_t *act;
+  F4 *partial;   // [parts][tiles][tokens][4]
   int32_t wide;  // hidden, rounded up to 16
+  int32_t parts;
+  int32_t most;  // entries, at most
 };
 
 struct Choices {
   int16_t expert[kTokens][kMaxChoices];  // -1: none
   float weight[kTokens][kMaxChoices];
-  uint32_t used[kMaxExperts / 32];  // of the local experts
-  int16_t list[kMaxExperts];
+  uint32_t tokens[kMaxExperts][2];  // of the local experts
+  // the entries: expert, with the number of tokens before in 16s above its 10
+  // bits, and row
+  int16_t list[kMaxEntries], rows[kMaxEntries];
   int32_t n;
 };
 
-__device__ __forceinline__ float load_logit(const void *p, int64_t i, int dtype) {
-  return dtype == TACCL_F32    ? ((const float *)p)[i]
-         : dtype == TACCL_BF16 ? (float)((const bf16_t *)p)[i]
-                               : (float)((const f16_t *)p)[i];
-}
-
-// The choices of the router (route.hip) for token t by a row of 16 lanes: the
-// largest logit k times, equal ones in the order of their index; minus infinity
-// and NaN never, a NaN in the sum of the exponentials.
-template <int kEpl>
+// The choices of the router (route.hip) for token t by kL lanes: the largest
+// logit k times, equal ones in the order of their index; minus infinity and NaN
+// never, a NaN in the sum of the exponentials.
+template <class T, int kL, int kEpl>
 __device__ __forceinline__ void choose(const taccl_ffn_tokens_t &a, int t, Choices &c) {
-  const int lane = threadIdx.x & 15, E = a.num_experts;
+  const int lane = threadIdx.x & (kL - 1), E = a.num_experts;
   const bool take = t < a.tokens && (!a.mask || a.mask[t]);
+  const T *row = (const T *)a.logits + t * a.logits_stride;
   float v[kEpl];
 #pragma unroll
   for (int i = 0; i < kEpl; i++) {
-    const int e = i * 16 + lane;
-    v[i] = take && e < E ? load_logit(a.logits, t * a.logits_stride + e, a.logits_dtype)
-                         : -__builtin_inff();
+    const int e = i * kL + lane;
+    v[i] = take && e < E ? (float)row[e] : -__builtin_inff();
   }
   float top = -__builtin_inff();
 #pragma unroll
   for (int i = 0; i < kEpl; i++) top = fmaxf(top, v[i]);
-  top = lanes_max<16>(top);
+  top = lanes_max<kL>(top);
   const float base = top == -__builtin_inff() ? 0.0f : top;
   float sum = 0;
 #pragma unroll
   for (int i = 0; i < kEpl; i++)
     sum += __builtin_amdgcn_exp2f((v[i] - base) * 1.4426950408889634f);
-  sum = lanes_sum<16>(sum);
+  sum = lanes_sum<kL>(sum);
   int own = -1;
   float p = 0;
   for (int j = 0; j < a.k; j++) {
     float m = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < kEpl; i++) m = fmaxf(m, v[i]);
-    m = lanes_max<16>(m);
+    m = lanes_max<kL>(m);
     uint32_t at = 0xFFFFFFFFu;
 #pragma unroll
-    for (int i = kEpl - 1; i >= 0; i--) at = v[i] == m ? (uint32_t)(i * 16 + lane) : at;
-    at = lanes_min<16>(at);
+    for (int i = kEpl - 1; i >= 0; i--) at = v[i] == m ? (uint32_t)(i * kL + lane) : at;
+    at = lanes_min<kL>(at);
     if (m == -__builtin_inff()) at = 0xFFFFFFFFu;
 #pragma unroll
-    for (int i = 0; i < kEpl; i++) v[i] = at == (uint32_t)(i * 16 + lane) ? -__builtin_inff() : v[i];
+    for (int i = 0; i < kEpl; i++)
+      v[i] = at == (uint32_t)(i * kL + lane) ? -__builtin_inff() : v[i];
     if (lane == j && at != 0xFFFFFFFFu) {
       own = (int)at;
       p = __builtin_amdgcn_exp2f((m - base) * 1.4426950408889634f);
     }
   }
-  if (a.renorm) sum = lanes_sum<16>(p);
+  if (a.renorm) sum = lanes_sum<kL>(p);
   if (t < a.tokens && lane < a.k) {
     c.expert[t][lane] = (int16_t)own;
     c.weight[t][lane] = own >= 0 ? p / sum : 0.0f;
     const int local = own - a.first_expert;
     if (own >= 0 && (uint32_t)local < (uint32_t)a.local_experts)
-      atomicOr(&c.used[local >> 5], 1u << (local & 31));
+      atomicOr(&c.tokens[local][t >> 5], 1u << (t & 31));
   }
 }
-
-// All tokens' choices and the list of chosen local experts, in their order
-__device__ __forceinline__ void choose_all(const taccl_ffn_tokens_t &a, Choices &c) {
-  for (int i = threadIdx.x; i < kMaxExperts / 32; i += blockDim.x) c.used[i] = 0;
-  __syncthreads();
-  for (int t0 = 0; t0 < a.tokens; t0 += blockDim.x / 16) {
-    const int t = t0 + threadIdx.x / 16;
-    if (t0 + (int)(threadIdx.x / 64) * 4 >= a.tokens) break;  // by wavefronts
-    if (a.num_experts <= 64) choose<4>(a, t, c);
-    else if (a.num_experts <= 256) choose<16>(a, t, c);
-    else choose<64>(a, t, c);
-  }
-  __syncthreads();
-  if (threadIdx.x < 64) {  // a word's experts per lane of the first half
-    uint32_t w = threadIdx.x < kMaxExperts / 32 ? c.used[threadIdx.x] : 0;
-    const uint32_t upto = wave_scan_add(__popc(w));
-    uint32_t at = upto - __popc(w);
-    for (; w; w &= w - 1) c.list[at++] = (int16_t)(threadIdx.x * 32 + __builtin_ctz(w));
-    if (threadIdx.x == 63) c.n = (int32_t)upto;
-  }
-  __syncthreads();
-}
-
-// Address of the chunk at hidden column f (a multiple of the chunk's) of a
-// token: float chunks, or pairs of 16-bit ones
+// a row of 16 lanes per token, past 256 experts a wavefront
 template <class T>
-__device__ __forceinline__ uint8_t *act_at(const TokensArgs &g, int slot, int t, int f) {
-  return g.act + ((int64_t)(slot * g.a.tokens + t) * g.wide + f) * 4;
+__device__ __forceinline__ void choose_each(const taccl_ffn_tokens_t &a, Choices &c) {
+  const int wave = threadIdx.x >> 6, row = threadIdx.x >> 4 & 3;
+  const int per = a.num_experts <= 256 ? 4 : 1;  // tokens of a wavefront
+  for (int t0 = wave * per; t0 < a.tokens; t0 += kWaves * per) {
+    if (a.num_experts <= 64) choose<T, 16, 4>(a, t0 + row, c);
+    else if (a.num_experts <= 256) choose<T, 16, 16>(a, t0 + row, c);
+    else choose<T, 64, 16>(a, t0, c);
+  }
 }
 
-// a of 16 hidden columns of an expert per turn: gate and up rows of its
-// weights, by eight wavefronts that take steps of 128 bytes in turn.
-template <class T, int NT, bool kTail>
-__global__ __launch_bounds__(64 * kUpWaves) void tokens_up_kernel(TokensArgs g) {
-  constexpr int N = Vec<T>::kN, U = NT == 1 ? 4 : 2;
+// All tokens' choices and the entries, in the experts' order
+__device__ __forceinline__ void choose_all(const taccl_ffn_tokens_t &a, Choices &c) {
+  for (int i = threadIdx.x; i < a.local_experts; i += kThreads) c.tokens[i][0] = c.tokens[i][1] = 0;
+  __syncthreads();
+  if (a.logits_dtype == TACCL_F32) choose_each<float>(a, c);
+  else if (a.logits_dtype == TACCL_BF16) choose_each<bf16_t>(a, c);
+  else choose_each<f16_t>(a, c);
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    uint32_t at = 0, row = 0;
+    for (int e0 = 0; e0 < a.local_experts; e0 += 64) {
+      const int e = e0 + threadIdx.x;
+      const uint32_t n =
+          e < a.local_experts ? __popc(c.tokens[e][0]) + __popc(c.tokens[e][1]) : 0;
+      // entries in the upper half of a word, rows in the lower
+      const uint32_t own = (n + 15) / 16 << 16 | n, upto = wave_scan_add(own);
+      uint32_t i = at + ((upto - own) >> 16), r = row + ((upto - own) & 0xFFFF);
+      for (uint32_t g = 0; g * 16 < n; g++, i++, r += 16) {
+        c.list[i] = (int16_t)(e | g << 10);
+        c.rows[i] = (int16_t)r;
+      }
+      const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+      at += all >> 16;
+      row += all & 0xFFFF;
+    }
+    if (threadIdx.x == 0) c.n = (int32_t)at;
+  }
+  __syncthreads();
+}
+
+// The n-th of the tokens, -1 without one
+__device__ __forceinline__ int token_of(const uint32_t *tokens, int n) {
+  const int low = __popc(tokens[0]);
+  uint32_t m = n < low ? tokens[0] : tokens[1];
+  int at = n < low ? 0 : 32;
+  n -= n < low ? 0 : low;
+  if (n >= __popc(m)) return -1;
+#pragma unroll
+  for (int w = 16; w; w /= 2) {
+    const int c = __popc(m & ((1u << w) - 1));
+    at += n >= c ? w : 0;
+    m = n >= c ? m >> w : m;
+    n -= n >= c ? c : 0;
+  }
+  return at;
+}
+
+// LDS writes of the block are done; loads from memory may be on their way
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// One operand's pieces of a step of 128 bytes (two products' worth) of a row of
+// K. The last step is moved back to end with the row, and what it has in common
+// with the one before is cleared by finish_step(); a row shorter than a step is
+// read in parts (kShort).
+template <class T>
+constexpr int kTokenStep = 8 * Vec<T>::kN;
+template <class T, bool kShort>
+__device__ __forceinline__ void load_step(Frag<T> *f, const T *p, int step, int K) {
+  constexpr int N = Vec<T>::kN;
+  const int q = threadIdx.x >> 4 & 3;
+  const int k0 = kShort ? 0 : min(step * kTokenStep<T>, K - kTokenStep<T>);
+#pragma unroll
+  for (int h = 0; h < 2; h++) {
+    const int k = k0 + (h * 4 + q) * N;
+    if (kShort) f[h].v = load_vec<T, true>(p + k, K - k);
+    else f[h].v = *(const typename Vec<T>::U *)(p + k);
+  }
+}
+template <class T, bool kShort>
+__device__ __forceinline__ void finish_step(Frag<T> *f, int step, int K) {
+  constexpr int N = Vec<T>::kN;
+  const int again = (step + 1) * kTokenStep<T> - K;  // elements in common
+  if (kShort || again <= 0) return;
+  const int q = threadIdx.x >> 4 & 3;
+#pragma unroll
+  for (int h = 0; h < 2; h++) {
+    Chunk v = __builtin_bit_cast(Chunk, f[h].v);
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int n = again - (h * 4 + q) * N - i * (N / 4);  // of this word's elements
+      v[i] &= n <= 0 ? ~0u : N == 8 && n == 1 ? 0xFFFF0000u : 0u;
+    }
+    f[h].v = __builtin_bit_cast(typename Vec<T>::V, v);
+  }
+}
+
+// w a of 8 hidden columns of an entry per turn: 8 gate and 8 up rows of its
+// expert's weights make one operand, its tokens the other; four wavefronts take
+// steps of 128 bytes in turn. The next steps are on their way while those
+// before are multiplied, across turns too.
+template <class T, bool kShort>
+__global__ __launch_bounds__(kThreads, kPerCu) void tokens_up_kernel(TokensArgs g) {
+  constexpr int U = 2;
   __shared__ Choices c;
-  __shared__ F4 red[kUpWaves][2][NT][64];
+  __shared__ F4 red[2][kWaves][64];
   const taccl_ffn_tokens_t &a = g.a;
-  const int D = a.cols, F = a.hidden, tiles = g.wide / 16;
+  const int D = a.cols, F = a.hidden, tiles = g.wide / 8;
   choose_all(a, c);
   if (blockIdx.x == 0) {
-    for (int i = threadIdx.x; i < a.tokens * a.k; i += blockDim.x) {
+    for (int i = threadIdx.x; i < a.tokens * a.k; i += kThreads) {
       if (a.experts) a.experts[i] = c.expert[i / a.k][i % a.k];
       if (a.weights) a.weights[i] = c.weight[i / a.k][i % a.k];
     }
-    for (int i = threadIdx.x; i < c.n; i += blockDim.x) g.chosen->experts[i] = c.list[i];
+    for (int i = threadIdx.x; i < c.n; i += kThreads) {
+      const int e = c.list[i] & (kMaxExperts - 1), from = (c.list[i] >> 10) * 16;
+      uint32_t some[2] = {c.tokens[e][0], c.tokens[e][1]};
+      // without the tokens before and behind
+      const int t0 = token_of(some, from), t1 = token_of(some, from + 16);
+      uint64_t m = (uint64_t)some[1] << 32 | some[0];
+      m &= ~0ull << t0;
+      if (t1 >= 0) m &= (1ull << t1) - 1;
+      g.chosen->tokens[i][0] = (uint32_t)m;
+      g.chosen->tokens[i][1] = (uint32_t)(m >> 32);
+      g.chosen->experts[i] = (int16_t)e;
+      g.chosen->rows[i] = c.rows[i];
+    }
+    for (int i = threadIdx.x; i < (D + 15) / 16; i += kThreads) g.chosen->done[i] = 0;
     if (threadIdx.x == 0) g.chosen->n = c.n;
   }
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
-  const int steps = (D + 8 * N - 1) / (8 * N);
-  for (int item = blockIdx.x; item < c.n * tiles; item += gridDim.x) {
-    const int slot = item / tiles, f0 = item % tiles * 16, e = c.list[slot];
-    const T *gate = (const T *)a.w_in + ((int64_t)e * 2 * F + min(f0 + r, F - 1)) * D;
-    const T *up = gate + (int64_t)F * D;
-    const T *x[NT];
-#pragma unroll
-    for (int i = 0; i < NT; i++)
-      x[i] = (const T *)a.x + min(16 * i + r, (int)a.tokens - 1) * a.x_stride;
-    F4 ag[NT], au[NT];
-#pragma unroll
-    for (int i = 0; i < NT; i++) ag[i] = au[i] = F4{0, 0, 0, 0};
-    for (int s0 = wave; s0 < steps; s0 += U * kUpWaves) {
-      Frag<T> fg[U][2], fu[U][2], fx[U][2][NT];
-#pragma unroll
-      for (int s = 0; s < U; s++)
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-          const int k = ((s0 + s * kUpWaves) * 8 + h * 4 + q) * N, left = D - k;
-          fg[s][h].v = load_vec<T, kTail>(gate + k, left);
-          fu[s][h].v = load_vec<T, kTail>(up + k, left);
-#pragma unroll
-          for (int i = 0; i < NT; i++) fx[s][h][i].v = load_vec<T, kTail>(x[i] + k, left);
-        }
-#pragma unroll
-      for (int s = 0; s < U; s++)
-#pragma unroll
-        for (int h = 0; h < 2; h++)
-#pragma unroll
-          for (int i = 0; i < NT; i++) {
-            ag[i] = multiply(fg[s][h], fx[s][h][i], ag[i]);
-            au[i] = multiply(fu[s][h], fx[s][h][i], au[i]);
-          }
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+  const int steps = (D + kTokenStep<T> - 1) / kTokenStep<T>;
+  const int batches = (steps + U * kWaves - 1) / (U * kWaves);
+
+  struct Batch {
+    Frag<T> w[U][2], x[U][2];
+  };
+  // the next batch to load: its turn, place in it and operands
+  int next = blockIdx.x, part = 0;
+  const T *w = nullptr, *x = nullptr;
+  auto load = [&](Batch &b) {
+    if (next >= c.n * tiles) return;
+    if (part == 0) {
+      const int entry = c.list[next / tiles], f = min(next % tiles * 8 + (r & 7), F - 1);
+      const int e = entry & (kMaxExperts - 1), t = token_of(c.tokens[e], (entry >> 10) * 16 + r);
+      w = (const T *)a.w_in + ((int64_t)e * 2 * F + (r < 8 ? f : F + f)) * D;
+      // columns without a token take the first one's row; they are not stored
+      x = (const T *)a.x + __shfl(t, t < 0 ? 0 : lane) * a.x_stride;
     }
 #pragma unroll
-    for (int i = 0; i < NT; i++) {
-      red[wave][0][i][lane] = ag[i];
-      red[wave][1][i][lane] = au[i];
+    for (int u = 0; u < U; u++) {
+      const int s = (part * U + u) * kWaves + wave;
+      if (s < steps) {
+        load_step<T, kShort>(b.w[u], w, s, D);
+        load_step<T, kShort>(b.x[u], x, s, D);
+      }
     }
-    __syncthreads();
-    // four hidden columns of a token per thread
-    const int t = 16 * wave + r, f = f0 + 4 * q;
-    if (wave < NT && t < a.tokens) {
-      F4 sg = red[0][0][wave][lane], su = red[0][1][wave][lane];
+    if (++part == batches) {
+      part = 0;
+      next += gridDim.x;
+    }
+  };
+  F4 acc = {0, 0, 0, 0};
+  int item = blockIdx.x, done = 0;
+  uint32_t turns = 0;
+  auto multiply_batch = [&](Batch &b) {
 #pragma unroll
-      for (int w = 1; w < kUpWaves; w++) {
-        sg += red[w][0][wave][lane];
-        su += red[w][1][wave][lane];
+    for (int u = 0; u < U; u++) {
+      const int s = (done * U + u) * kWaves + wave;
+      if (s < steps) {
+        finish_step<T, kShort>(b.w[u], s, D);
+        finish_step<T, kShort>(b.x[u], s, D);
+#pragma unroll
+        for (int h = 0; h < 2; h++) acc = multiply(b.w[u][h], b.x[u][h], acc);
+      }
+    }
+    if (++done < batches) return;
+    done = 0;
+    const uint32_t turn = turns & 1;
+    red[turn][wave][lane] = acc;
+    acc = F4{0, 0, 0, 0};
+    const int f = item % tiles * 8 + 4 * q, slot = item / tiles;
+    item += gridDim.x;
+    lds_barrier();
+    // the turns' sums go to the wavefronts in turn: lanes 0 to 31 take four
+    // hidden columns of a token, whose gate rows they and whose up rows lanes 32
+    // to 63 held
+    const int e = c.list[slot] & (kMaxExperts - 1);
+    const int t = q < 2 && wave == (int)(turns & (kWaves - 1))
+                      ? token_of(c.tokens[e], (c.list[slot] >> 10) * 16 + r) : -1;
+    if (t >= 0) {
+      F4 sg = red[turn][0][lane], su = red[turn][0][lane + 32];
+#pragma unroll
+      for (int v = 1; v < kWaves; v++) {
+        sg += red[turn][v][lane];
+        su += red[turn][v][lane + 32];
       }
       float weight = 0;
-      bool member = false;
       for (int j = 0; j < a.k; j++)
-        if (c.expert[t][j] == e + a.first_expert) {
-          member = true;
-          weight = c.weight[t][j];
-        }
+        if (c.expert[t][j] == e + a.first_expert) weight = c.weight[t][j];
       F4 y;
 #pragma unroll
       for (int i = 0; i < 4; i++) {
@@ -222,10 +332,11 @@ __global__ __launch_bounds__(64 * kUpWaves) void tokens_up_kernel(TokensArgs g) 
                             ? 1.0f / (1.0f + expf(-sg[i]))
                             : __builtin_amdgcn_rcpf(
                                   1.0f + __builtin_amdgcn_exp2f(sg[i] * -1.4426950408889634f));
-        y[i] = member && f + i < F ? sg[i] * s * su[i] * weight : 0.0f;
+        y[i] = f + i < F ? sg[i] * s * su[i] * weight : 0.0f;
       }
+      T *row = (T *)(g.act + (int64_t)(c.rows[slot] + r) * g.wide * 4) + f;
       if constexpr (sizeof(T) == 4) {
-        *(F4 *)act_at<T>(g, slot, t, f) = y;
+        *(F4 *)row = y;
       } else {
         typedef T T4 __attribute__((ext_vector_type(4)));
         T4 hi, lo;
@@ -235,66 +346,179 @@ __global__ __launch_bounds__(64 * kUpWaves) void tokens_up_kernel(TokensArgs g) 
           const float rest = y[i] - (float)hi[i];
           lo[i] = (T)(rest - rest == 0 ? rest : 0.0f);  // not of an infinite number
         }
-        uint8_t *p = act_at<T>(g, slot, t, f & ~7) + (f & 4) * 2;
-        *(T4 *)p = hi;
-        *(T4 *)(p + 16) = lo;
+        *(T4 *)row = hi;
+        *(T4 *)(row + g.wide) = lo;
       }
     }
-    __syncthreads();
+    turns++;  // the other half's readers are behind this turn's barrier
+  };
+  Batch even, odd;
+  load(even);
+  const int end = c.n * tiles;
+  while (item < end) {
+    load(odd);
+    multiply_batch(even);
+    if (item >= end) break;
+    load(even);
+    multiply_batch(odd);
   }
 }
 
-// 16 columns of the output: the chosen experts' rows of w_out one after the
-// other as one long shared axis.
-template <class T, int NT, bool kTail>
-__global__ __launch_bounds__(64 * kDownWaves) void tokens_down_kernel(TokensArgs g) {
-  constexpr int N = Vec<T>::kN, U = NT == 1 ? 2 : 1, kPlanes = sizeof(T) == 4 ? 1 : 2;
-  __shared__ F4 red[kDownWaves][NT][64];
+// Stores and loads that other XCDs' blocks see and have made
+__device__ __forceinline__ void put(float *p, F4 v) {
+#pragma unroll
+  for (int i = 0; i < 4; i++)
+    __hip_atomic_store(p + i, v[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ F4 get(const float *p) {
+  F4 v;
+#pragma unroll
+  for (int i = 0; i < 4; i++)
+    v[i] = __hip_atomic_load(p + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return v;
+}
+
+// 16 columns of the output, or a part of their sum: the entries' rows of w_out
+// one after the other are one long shared axis, dealt out to parts where the
+// columns alone make too few blocks. The last part to arrive adds them up, in
+// their order. Up to 16 tokens a column of the operand is a token; more are
+// added up per wavefront in LDS, entry by entry (kMany).
+template <class T, bool kMany, bool kShort>
+__global__ __launch_bounds__(kThreads, kDownPerCu<T>) void tokens_down_kernel(TokensArgs g) {
+  constexpr int U = 2, kPlanes = sizeof(T) == 4 ? 1 : 2;
+  constexpr int kCols = kMany ? kTokens : 16;
+  __shared__ F4 sums[kWaves][kCols][4];
+  __shared__ uint32_t tokens[kMaxEntries][2];
+  __shared__ int16_t experts[kMaxEntries], rows[kMaxEntries];
+  __shared__ int last;
   const taccl_ffn_tokens_t &a = g.a;
-  const int D = a.cols, F = a.hidden;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
-  const int d0 = blockIdx.x * 16, steps = (F + 8 * N - 1) / (8 * N), n = g.chosen->n;
-  F4 acc[NT];
+  const int D = a.cols, F = a.hidden, n = g.chosen->n;
+  // those past the n-th are not used: n is on its way too
+  for (int i = threadIdx.x; i < g.most; i += kThreads) {
+    tokens[i][0] = g.chosen->tokens[i][0];
+    tokens[i][1] = g.chosen->tokens[i][1];
+    rows[i] = g.chosen->rows[i];
+    experts[i] = g.chosen->experts[i];
+  }
+  for (int i = threadIdx.x; i < kWaves * kCols * 4; i += kThreads)
+    (&sums[0][0][0])[i] = F4{0, 0, 0, 0};
+  __syncthreads();
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+  const int tile = blockIdx.x / g.parts, part = blockIdx.x % g.parts, d0 = tile * 16;
+  const int steps = (F + kTokenStep<T> - 1) / kTokenStep<T>;
+
+  struct Batch {
+    Frag<T> w[U][2], x[U][kPlanes][2];
+    int slot[U], step[U];
+  };
+  const T *first = (const T *)a.w_out + (int64_t)min(d0 + r, D - 1) * F;
+  // every kWaves-th of the part's steps
+  const int64_t all = (int64_t)n * steps, from = all * part / g.parts + wave;
+  const int64_t end = all * (part + 1) / g.parts;
+  const int count = from < end ? (int)((end - from + kWaves - 1) / kWaves) : 0;
+  int slot = count ? (int)(from / steps) : 0, s = count ? (int)(from % steps) : 0;
+  int loaded = 0, done = 0;
+  auto load = [&](Batch &b) {
 #pragma unroll
-  for (int i = 0; i < NT; i++) acc[i] = F4{0, 0, 0, 0};
-  for (int s0 = wave; s0 < n * steps; s0 += U * kDownWaves) {
-    Frag<T> fw[U][2], fa[U][2][NT][kPlanes];
+    for (int u = 0; u < U; u++) {
+      if (loaded + u >= count) continue;
+      b.slot[u] = slot;
+      b.step[u] = s;
+      load_step<T, kShort>(b.w[u], first + (int64_t)experts[slot] * D * F, s, F);
+      // the token's row, or zeros
+      int row;
+      bool there;
+      const uint32_t low = tokens[slot][0], high = tokens[slot][1];
+      if (kMany) {
+        there = r < __popc(low) + __popc(high);
+        row = rows[slot] + r;
+      } else {
+        there = low >> r & 1;
+        row = rows[slot] + __popc(low & ((1u << r) - 1));
+      }
 #pragma unroll
-    for (int s = 0; s < U; s++) {
-      const int step = s0 + s * kDownWaves, slot = min(step / steps, n - 1);
-      const int e = g.chosen->experts[slot];
-      const T *w = (const T *)a.w_out + ((int64_t)e * D + min(d0 + r, D - 1)) * F;
-#pragma unroll
-      for (int h = 0; h < 2; h++) {
-        const int k = (step % steps * 8 + h * 4 + q) * N;
-        const int left = step < n * steps ? F - k : 0;
-        fw[s][h].v = load_vec<T, kTail>(w + k, left);
-#pragma unroll
-        for (int i = 0; i < NT; i++)
-#pragma unroll
-          for (int p = 0; p < kPlanes; p++) {
-            const uint8_t *at = act_at<T>(g, slot, min(16 * i + r, (int)a.tokens - 1), k) + 16 * p;
-            fa[s][h][i][p].v = load_vec<T, false>((const T *)at, left > 0 ? N : 0);
-          }
+      for (int p = 0; p < kPlanes; p++) {
+        b.x[u][p][0].v = b.x[u][p][1].v = typename Vec<T>::V{};
+        if (there)
+          load_step<T, kShort>(b.x[u][p], (const T *)(g.act + (int64_t)row * g.wide * 4) + p * g.wide,
+                               s, F);
+      }
+      s += kWaves;
+      while (s >= steps) {
+        s -= steps;
+        slot++;
       }
     }
+    loaded += U;
+  };
+  F4 acc = {0, 0, 0, 0};
+  int now = count ? slot : 0;  // the entry that acc belongs to
+  auto flush = [&]() {
+    const int t = token_of(tokens[now], r);
+    if (t >= 0) sums[wave][t][q] += acc;
+    acc = F4{0, 0, 0, 0};
+  };
+  auto multiply_batch = [&](Batch &b) {
 #pragma unroll
-    for (int s = 0; s < U; s++)
+    for (int u = 0; u < U; u++) {
+      if (done + u >= count) continue;
+      if (kMany && b.slot[u] != now) {
+        flush();
+        now = b.slot[u];
+      }
+      finish_step<T, kShort>(b.w[u], b.step[u], F);
 #pragma unroll
-      for (int h = 0; h < 2; h++)
+      for (int p = 0; p < kPlanes; p++) {
+        finish_step<T, kShort>(b.x[u][p], b.step[u], F);
 #pragma unroll
-        for (int i = 0; i < NT; i++)
-#pragma unroll
-          for (int p = 0; p < kPlanes; p++) acc[i] = multiply(fw[s][h], fa[s][h][i][p], acc[i]);
+        for (int h = 0; h < 2; h++) acc = multiply(b.w[u][h], b.x[u][p][h], acc);
+      }
+    }
+    done += U;
+  };
+  Batch even, odd;
+  load(even);
+  while (done < count) {
+    load(odd);
+    multiply_batch(even);
+    load(even);
+    multiply_batch(odd);
   }
-#pragma unroll
-  for (int i = 0; i < NT; i++) red[wave][i][lane] = acc[i];
+  if (!kMany) sums[wave][r][q] = acc;
+  else if (count) flush();
   __syncthreads();
-  const int t = 16 * wave + r, d = d0 + 4 * q;
-  if (wave < NT && t < a.tokens) {
-    F4 y = red[0][wave][lane];
+
+  // thread (t, c): four columns of a token
+  const int t = threadIdx.x >> 2, c = threadIdx.x & 3;
+  const bool own = t < a.tokens;
+  F4 y = {0, 0, 0, 0};
+  if (own) {
+    y = sums[0][t][c];
 #pragma unroll
-    for (int w = 1; w < kDownWaves; w++) y += red[w][wave][lane];
+    for (int v = 1; v < kWaves; v++) y += sums[v][t][c];
+  }
+  if (g.parts > 1) {
+    const int64_t stride = (int64_t)(gridDim.x / g.parts) * a.tokens * 4;
+    float *partial = (float *)(g.partial + ((int64_t)tile * a.tokens + t) * 4 + c);
+    if (own) put(partial + part * stride * 4, y);
+    // the parts are there (atomic stores of the device's scope, waited for)
+    // before they are counted; fences, which write back and drop an L2, took
+    // ten times as long as the product
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0)
+      last = __hip_atomic_fetch_add(&g.chosen->done[tile], 1, __ATOMIC_RELAXED,
+                                    __HIP_MEMORY_SCOPE_AGENT) == g.parts - 1;
+    __syncthreads();
+    if (!last) return;
+    if (own) {
+      y = get(partial);
+      for (int p = 1; p < g.parts; p++) y += get(partial + p * stride * 4);
+    }
+  }
+  if (own) {
+    const int d = d0 + 4 * c;
     T *out = (T *)a.out + t * a.out_stride + d;
 #pragma unroll
     for (int i = 0; i < 4; i++)
@@ -302,40 +526,57 @@ __global__ __launch_bounds__(64 * kDownWaves) void tokens_down_kernel(TokensArgs
   }
 }
 
-template <class T, bool kTail>
-const void *tokens_fn(int tokens, bool up) {
-#define F(NT)                                            \
-  (up ? (const void *)tokens_up_kernel<T, NT, kTail>     \
-      : (const void *)tokens_down_kernel<T, NT, kTail>)
-  return tokens <= 16 ? F(1) : tokens <= 32 ? F(2) : F(4);
-#undef F
+template <class T>
+const void *up_fn(int cols) {
+  return cols < kTokenStep<T> ? (const void *)tokens_up_kernel<T, true>
+                              : (const void *)tokens_up_kernel<T, false>;
 }
-const void *tokens_fn(int dtype, int tokens, bool tail, bool up) {
-#define F(T) (tail ? tokens_fn<T, true>(tokens, up) : tokens_fn<T, false>(tokens, up))
-  return dtype == TACCL_F32 ? F(float) : dtype == TACCL_BF16 ? F(bf16_t) : F(f16_t);
-#undef F
+template <class T>
+const void *down_fn(int hidden, bool many) {
+  const bool brief = hidden < kTokenStep<T>;
+  return many ? (brief ? (const void *)tokens_down_kernel<T, true, true>
+                       : (const void *)tokens_down_kernel<T, true, false>)
+              : (brief ? (const void *)tokens_down_kernel<T, false, true>
+                       : (const void *)tokens_down_kernel<T, false, false>);
+}
+
+int64_t act_bytes(int64_t tokens, int64_t k, int64_t hidden) {
+  return tokens * k * hidden_wide(hidden) * 4;
 }
 
 }  // namespace
 
-int64_t ffn_tokens_space(int64_t tokens, int64_t experts, int64_t k, int64_t hidden) {
-  return kChosenBytes + std::min(experts, tokens * k) * tokens * hidden_wide(hidden) * 4;
+int64_t ffn_tokens_space(int64_t tokens, int64_t k, int64_t cols, int64_t hidden) {
+  return kChosenBytes + act_bytes(tokens, k, hidden) +
+         kMaxParts * ((cols + 15) / 16) * tokens * 64;
 }
 
 hipError_t launch_ffn_tokens(const taccl_ffn_tokens_t &a, int cus, hipStream_t stream) {
-  TokensArgs g{a, (Chosen *)a.workspace, (uint8_t *)a.workspace + kChosenBytes,
-               (int32_t)hidden_wide(a.hidden)};
-  const int n = a.dtype == TACCL_F32 ? 4 : 8;
+  uint8_t *ws = (uint8_t *)a.workspace;
+  TokensArgs g{a, (Chosen *)ws, ws + kChosenBytes, nullptr, (int32_t)hidden_wide(a.hidden), 1, 0};
+  g.partial = (F4 *)(g.act + act_bytes(a.tokens, a.k, a.hidden));
   void *args[] = {&g};
-  const int64_t items =
-      std::min<int64_t>(a.local_experts, a.tokens * a.k) * (g.wide / 16);
-  hipError_t e = hipLaunchKernel(tokens_fn(a.dtype, (int)a.tokens, a.cols % n != 0, true),
-                                 dim3((uint32_t)std::min<int64_t>(items, 2 * cus)),
-                                 dim3(64 * kUpWaves), args, 0, stream);
+#define BY_TYPE(F, ...)                              \
+  (a.dtype == TACCL_F32    ? F<float>(__VA_ARGS__)   \
+   : a.dtype == TACCL_BF16 ? F<bf16_t>(__VA_ARGS__)  \
+                           : F<f16_t>(__VA_ARGS__))
+  // entries, at most
+  const int64_t choices = a.tokens * a.k;
+  const int64_t most = std::min<int64_t>(choices, a.local_experts + choices / 16);
+  const int64_t blocks = std::min<int64_t>(most * (g.wide / 8), kPerCu * cus);
+  g.most = (int32_t)most;
+  hipError_t e = hipLaunchKernel(BY_TYPE(up_fn, a.cols), dim3((uint32_t)blocks), dim3(kThreads),
+                                 args, 0, stream);
   if (e != hipSuccess) return e;
-  return hipLaunchKernel(tokens_fn(a.dtype, (int)a.tokens, a.hidden % n != 0, false),
-                         dim3((uint32_t)(a.cols + 15) / 16), dim3(64 * kDownWaves), args, 0,
-                         stream);
+  // parts of at least four steps per wavefront, if that many entries are there
+  const int n = a.dtype == TACCL_F32 ? 4 : 8;
+  const int64_t tiles = (a.cols + 15) / 16, steps = most * ((a.hidden + 8 * n - 1) / (8 * n));
+  const int64_t held = (a.dtype == TACCL_F32 ? kDownPerCu<float> : kDownPerCu<bf16_t>) * cus;
+  g.parts = (int)std::max<int64_t>(
+      1, std::min<int64_t>({held / tiles, steps / (4 * kWaves), kMaxParts}));
+  return hipLaunchKernel(BY_TYPE(down_fn, a.hidden, a.tokens > 16),
+                         dim3((uint32_t)(tiles * g.parts)), dim3(kThreads), args, 0, stream);
+#undef BY_TYPE
 }
 
 }  // namespace taccl

@@ -75,12 +75,11 @@ def ffn_workspace(shape, hidden, dtype, backward=False):
                  types=[ct.c_int32, ct.c_int32, ct.c_int64] + [ct.c_int32] * 3)
 
 
-def ffn_tokens_workspace(tokens, num_experts, k, hidden):
-    """Bytes of ffn_tokens_tensors' workspace; num_experts are those that its
-    weights hold. 0 for sizes that it refuses."""
-    if not _fits(tokens, num_experts, k, hidden):
+def ffn_tokens_workspace(tokens, k, dim, hidden):
+    """Bytes of ffn_tokens_tensors' workspace; 0 for sizes that it refuses."""
+    if not _fits(tokens, k, dim, hidden):
         return 0
-    return _size("taccl_ffn_tokens_workspace", tokens, num_experts, k, hidden,
+    return _size("taccl_ffn_tokens_workspace", tokens, k, dim, hidden,
                  types=[ct.c_int64] + [ct.c_int32] * 3)
 
 
@@ -398,7 +397,7 @@ class _FfnTokensFn(torch.autograd.Function):
         out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         experts = torch.empty(len(x), k, dtype=torch.int32, device=x.device)
         weights = torch.empty(len(x), k, device=x.device)
-        size = ffn_tokens_workspace(len(x), len(w_out), k, w_out.shape[2])
+        size = ffn_tokens_workspace(len(x), k, x.shape[1], w_out.shape[2])
         ffn_tokens_tensors(x, logits, w_in, w_out, out, _workspace(size, x), k=k, mask=mask,
                            renorm=renorm, first_expert=first_expert, experts=experts,
                            weights=weights)

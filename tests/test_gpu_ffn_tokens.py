@@ -30,7 +30,7 @@ def run(m, k, **options):
     out = torch.full((t, d + 3), 7.0, dtype=m["x"].dtype, device="cuda")
     experts = torch.full((t, k), -9, dtype=torch.int32, device="cuda")
     weights = torch.full((t, k), float("nan"), device="cuda")
-    n = X.ffn_tokens_workspace(t, len(m["w_out"]), k, m["w_out"].shape[2])
+    n = X.ffn_tokens_workspace(t, k, d, m["w_out"].shape[2])
     work = torch.full((n + 256,), 0xFF, dtype=torch.uint8, device="cuda")  # NaN in every type
     X.ffn_tokens_tensors(m["x"], m["logits"], m["w_in"], m["w_out"], out[:, :d], work[:n], k=k,
                          experts=experts, weights=weights, **options)
