@@ -572,8 +572,9 @@ taccl_status_t taccl_combine_backward(const taccl_combine_backward_t *a, taccl_s
  * is infinite. Sums run over 32-bit floats; for TACCL_F32 too every product is
  * one of 32-bit floats. Arrays are contiguous.
  * 1 <= sources, E <= 1024, 1 <= cols, hidden <= 65536, 1 <= capacity, sources *
- * capacity <= 2^21, sources * E * capacity < 2^31, and fewer than 2^23 tiles of
- * 64 rows by 64 columns. cols and hidden in whole 16-byte units and arrays on
+ * capacity <= 2^21, sources * E * capacity < 2^31, and fewer than 2^23 tiles: E
+ * (R (H + C) + 2 C H) for R = sources * capacity / 32, H = hidden / 32 and C =
+ * cols / 64, each rounded up. cols and hidden in whole 16-byte units and arrays on
  * 16 bytes are fastest. `workspace`: taccl_ffn_workspace(sources, E, capacity,
  * hidden, dtype, backward) bytes, 16-byte aligned, not shared with another call
  * in flight.

@@ -85,11 +85,12 @@ void check_ffn_sizes(Check &c, const FfnSizes &z) {
   c.invalid(z.cols < 1 || z.hidden < 1, "cols and hidden must be at least 1");
   c.limit(z.cols > kFfnMaxCols || z.hidden > kFfnMaxCols, "more than 65536 columns");
   if (c.st) return;
-  // blocks of the largest grid, whose threads have to stay below 2^32
+  // blocks of the largest grid (the gradient's last one, of the smallest tiles),
+  // whose threads have to stay below 2^32
   auto tiles = [](int64_t n) { return (n + 63) / 64; };
-  const int64_t rows = tiles(z.sources * z.capacity), wide = tiles(2 * z.hidden);
-  const int64_t most = std::max({rows * wide, rows * tiles(z.cols), tiles(z.cols) * wide});
-  c.limit(z.experts * most >= 1 << 23, "2^23 tiles of 64 x 64 or more");
+  const int64_t rows = (z.sources * z.capacity + 31) / 32, wide = tiles(2 * z.hidden);
+  const int64_t all = rows * (wide + tiles(z.cols)) + tiles(z.cols) * 2 * wide;
+  c.limit(z.experts * all >= 1 << 23, "2^23 tiles or more");
 }
 template <class A>
 void check_ffn(Check &c, const A &a, bool backward) {

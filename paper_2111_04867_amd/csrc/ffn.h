@@ -20,8 +20,8 @@ constexpr int kDropoutMaxCols = 1 << 20;
 // e * sources * capacity on.
 struct FfnSpace {
   int64_t rows;       // int32 [E]: rows of each expert
-  int64_t num_tiles;  // int32 [1]
-  int64_t tiles;      // FfnTile[]
+  int64_t num_tiles;  // int32 [4]
+  int64_t tiles[4];   // FfnTile[]: tiles of 32, 64, 128 and 256 rows
   int64_t map;        // int32 [E][sources * capacity]: row numbers in the buffer (sources > 1)
   int64_t act;        // T [E][sources * capacity][hidden]
   int64_t dpre;       // T [E][sources * capacity][2 hidden] (backward)

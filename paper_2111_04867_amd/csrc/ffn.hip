@@ -14,6 +14,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "expert.h"
 #include "ffn.h"
 #include "tile.h"
 
@@ -29,7 +30,10 @@ constexpr int kPlanThreads = 256;
 
 int64_t rounded(int64_t n) { return (n + 255) / 256 * 256; }
 
-constexpr int kMinTile = 64;  // rows of the smallest tile, for the list's length
+// rows of a tile: each size has its own list, 2^(5 + i) rows in list i
+constexpr int kLists = 4;
+constexpr int64_t list_rows(int i) { return 32 << i; }
+constexpr int list_of(int rows) { return rows == 256 ? 3 : rows == 128 ? 2 : rows == 64 ? 1 : 0; }
 
 }  // namespace
 
@@ -39,8 +43,12 @@ FfnSpace ffn_space(int64_t sources, int64_t experts, int64_t capacity, int64_t h
   const int64_t size = dtype == TACCL_F32 ? 4 : 2;
   FfnSpace s{};
   s.num_tiles = rounded(4 * experts);
-  s.tiles = s.num_tiles + 256;
-  s.map = s.tiles + rounded(8 * experts * ((slots + kMinTile - 1) / kMinTile));
+  int64_t at = s.num_tiles + 256;
+  for (int i = 0; i < kLists; i++) {
+    s.tiles[i] = at;
+    at += rounded(8 * experts * ((slots + list_rows(i) - 1) / list_rows(i)));
+  }
+  s.map = at;
   s.act = s.map + (sources > 1 ? rounded(4 * rows) : 0);
   s.dpre = s.act + rounded(rows * hidden * size);
   s.bytes = s.dpre + (backward ? rounded(2 * rows * hidden * size) : 0);
@@ -52,15 +60,17 @@ namespace {
 struct PlanArgs {
   const int32_t *counts;  // [S][E]
   int64_t capacity;
-  int32_t sources, experts, tile, parts;
+  int32_t sources, experts;
+  int32_t map_parts, zero_parts;  // blocks per expert, per source and expert
   int32_t *rows, *num_tiles, *map;  // map: or null
-  FfnTile *tiles;
+  FfnTile *tiles[kLists];
+  int32_t lists;  // bits: those that a product reads
   uint8_t *zero;  // rows past the counts are zeroed; or null
   int64_t row_bytes;
 };
 
-__device__ __forceinline__ int64_t rows_of(const PlanArgs &g, int s, int e) {
-  return min((int64_t)max(g.counts[(int64_t)s * g.experts + e], 0), g.capacity);
+__device__ __forceinline__ int32_t rows_of(const PlanArgs &g, int64_t i) {
+  return (int32_t)min((int64_t)max(g.counts[i], 0), g.capacity);
 }
 
 // Inclusive sum over the block's threads of v; `all` becomes the total
@@ -79,59 +89,78 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t *red, uint32
   return own + before;
 }
 
-// Block 0 counts and lists, the others number and zero the rows of an expert.
+// Block 0 counts and lists; then come the blocks that number an expert's rows
+// and those that zero a source's rows of an expert.
 __global__ __launch_bounds__(kPlanThreads) void ffn_plan_kernel(PlanArgs g) {
   __shared__ uint32_t red[kPlanThreads / 64];
+  __shared__ int32_t rows[kMaxExperts];
+  __shared__ uint32_t from[kMaxExperts + 1];  // an expert's first tile, a source's first row
+  const int E = g.experts, S = g.sources;
   if (blockIdx.x == 0) {
-    uint32_t first = 0;
-    for (int e0 = 0; e0 < g.experts; e0 += kPlanThreads) {
-      const int e = e0 + threadIdx.x;
-      int64_t n = 0;
-      if (e < g.experts) {
-        for (int s = 0; s < g.sources; s++) n += rows_of(g, s, e);
-        g.rows[e] = (int32_t)n;
+    for (int e = threadIdx.x; e < E; e += kPlanThreads) rows[e] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < S * E; i += kPlanThreads) atomicAdd(&rows[i % E], rows_of(g, i));
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += kPlanThreads) g.rows[e] = rows[e];
+    for (int l = 0; l < kLists; l++) {
+      if (!(g.lists >> l & 1)) continue;
+      const uint32_t tile = (uint32_t)list_rows(l);
+      uint32_t total = 0;
+      for (int e0 = 0; e0 < E; e0 += kPlanThreads) {
+        const int e = e0 + threadIdx.x;
+        const uint32_t mine = e < E ? ((uint32_t)rows[e] + tile - 1) / tile : 0;
+        uint32_t all;
+        const uint32_t upto = total + block_scan(mine, red, all);
+        if (e < E) from[e + 1] = upto;
+        total += all;
       }
-      const uint32_t mine = (uint32_t)((n + g.tile - 1) / g.tile);
-      uint32_t all;
-      const uint32_t at = first + block_scan(mine, red, all) - mine;
-      for (uint32_t i = 0; i < mine; i++)
-        g.tiles[at + i] = FfnTile{e, (int32_t)(i * (uint32_t)g.tile)};
-      first += all;
+      if (threadIdx.x == 0) {
+        from[0] = 0;
+        g.num_tiles[l] = (int32_t)total;
+      }
+      __syncthreads();
+      for (uint32_t i = threadIdx.x; i < total; i += kPlanThreads) {
+        int e = 0;  // the last expert whose first tile is not behind i, among those with tiles
+        for (int n = E; n > 1; n = (n + 1) / 2)
+          if (e + n / 2 < E && from[e + n / 2] <= i) e += n / 2;
+        g.tiles[l][i] = FfnTile{e, (int32_t)((i - from[e]) * tile)};
+      }
+      __syncthreads();
     }
-    if (threadIdx.x == 0) *g.num_tiles = (int32_t)first;
     return;
   }
-  const int b = blockIdx.x - 1, e = b % g.experts, part = b / g.experts;
-  const int64_t slots = g.sources * g.capacity;
-  if (g.map) {
-    int32_t *map = g.map + e * slots;
+  int b = blockIdx.x - 1;
+  if (b < E * g.map_parts) {
+    const int e = b % E, part = b / E;
+    int32_t *map = g.map + e * S * g.capacity;
     uint32_t first = 0;
-    for (int s0 = 0; s0 < g.sources; s0 += kPlanThreads) {
+    for (int s0 = 0; s0 < S; s0 += kPlanThreads) {
       const int s = s0 + threadIdx.x;
-      const uint32_t n = s < g.sources ? (uint32_t)rows_of(g, s, e) : 0;
+      const uint32_t n = s < S ? (uint32_t)rows_of(g, (int64_t)s * E + e) : 0;
       uint32_t all;
-      const uint32_t at = first + block_scan(n, red, all) - n;
-      // each source's rows by the whole block, one source after the other
-      __shared__ uint32_t from[kPlanThreads], len[kPlanThreads];
-      from[threadIdx.x] = at;
-      len[threadIdx.x] = n;
+      const uint32_t upto = block_scan(n, red, all);
+      if (threadIdx.x == 0) from[0] = 0;
+      from[threadIdx.x + 1] = upto;
       __syncthreads();
-      for (int i = 0; i < min(kPlanThreads, g.sources - s0); i++) {
-        const int64_t row = ((int64_t)(s0 + i) * g.experts + e) * g.capacity;
-        for (uint32_t j = part * kPlanThreads + threadIdx.x; j < len[i];
-             j += g.parts * kPlanThreads)
-          map[from[i] + j] = (int32_t)(row + j);
+      // the rows of these sources, a row per thread and turn
+      for (uint32_t i = part * kPlanThreads + threadIdx.x; i < all;
+           i += g.map_parts * kPlanThreads) {
+        int at = 0;
+#pragma unroll
+        for (int n = kPlanThreads / 2; n; n /= 2)
+          if (from[at + n] <= i) at += n;
+        map[first + i] = (int32_t)(((int64_t)(s0 + at) * E + e) * g.capacity + (i - from[at]));
       }
       first += all;
+      __syncthreads();
     }
+    return;
   }
-  if (g.zero) {
-    for (int s = 0; s < g.sources; s++) {
-      const int64_t n = rows_of(g, s, e), row = ((int64_t)s * g.experts + e) * g.capacity + n;
-      zero_piece<kPlanThreads>(g.zero + row * g.row_bytes, (g.capacity - n) * g.row_bytes, part,
-                               g.parts);
-    }
-  }
+  b -= E * g.map_parts;
+  const int i = b % (S * E), part = b / (S * E);
+  const int64_t n = rows_of(g, i);
+  zero_piece<kPlanThreads>(g.zero + (i * g.capacity + n) * g.row_bytes,
+                           (g.capacity - n) * g.row_bytes, part, g.zero_parts);
 }
 
 // The products. kUp: a from x and w_in (and the stored g, u); kDown: y from a
@@ -158,49 +187,26 @@ __device__ __forceinline__ float sigmoid(float g) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f));
 }
 
-// Four results of a row; `left` columns of it exist
-template <class T, bool kFast>
-__device__ __forceinline__ void store_four(T *p, F4 v, int left) {
-  typedef T T4 __attribute__((ext_vector_type(4)));
-  if (kFast) {
-    if (left > 0) *(T4 *)p = T4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; i++)
-      if (i < left) p[i] = (T)v[i];
-  }
-}
-template <class T, bool kFast>
-__device__ __forceinline__ F4 load_four(const T *p, int left) {
-  typedef T T4 __attribute__((ext_vector_type(4)));
-  F4 v = {0, 0, 0, 0};
-  if (kFast) {
-    if (left > 0) {
-      const T4 t = *(const T4 *)p;
-#pragma unroll
-      for (int i = 0; i < 4; i++) v[i] = (float)t[i];
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; i++)
-      if (i < left) v[i] = (float)p[i];
-  }
-  return v;
-}
+// A tile of BM rows by BN columns, by WM x WN wavefronts, over steps of kBytes
+// bytes of the shared axis, of which S lie in LDS.
+template <int M, int N, int kM, int kN, int B, int kS>
+struct Shape {
+  static constexpr int BM = M, BN = N, WM = kM, WN = kN, kBytes = B, S = kS;
+  static constexpr int kThreads = 64 * WM * WN, kLds = S * (BM + BN) * kBytes;
+};
 
-// A tile of BM rows by BN columns; WM x WN wavefronts.
-template <class T, int kKind, bool kFast, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void ffn_product_kernel(ProductArgs g) {
+template <class T, int kKind, bool kMapped, bool kFast, class Z>
+__device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *lds) {
   constexpr bool kWeights = kKind == kDwOut || kKind == kDwIn;
   constexpr bool kAcrossA = kWeights, kAcrossB = kKind != kUp && kKind != kDown;
-  constexpr int kThreads = 64 * WM * WN, MI = BM / WM / 16, NI = BN / WN / 16;
-  constexpr int kBuffer = (BM + BN) * kStepBytes;
-  extern __shared__ __align__(16) char lds[];
+  constexpr int BM = Z::BM, BN = Z::BN, WM = Z::WM, WN = Z::WN, kBytes = Z::kBytes, S = Z::S;
+  constexpr int kThreads = Z::kThreads, MI = BM / WM / 16, NI = BN / WN / 16;
+  constexpr int kBuffer = (BM + BN) * kBytes, kTileA = BM * kBytes;
   const int D = g.cols, F = g.hidden;
 
   // Blocks go to the XCDs in turn; 32 consecutive ones of an XCD take a piece
   // of 8 tiles of columns by 4 of rows, whose operands its L2 holds.
-  const uint32_t b = blockIdx.x, per_xcd = b >> 3;
+  const uint32_t per_xcd = b >> 3;
   const uint32_t id = ((per_xcd >> 5) * 8 + (b & 7)) * 32 + (per_xcd & 31);
   const uint32_t entries = kWeights ? (uint32_t)(g.experts * g.row_tiles) : (uint32_t)*g.num_tiles;
   const uint32_t group = id / (entries * 8), width = min(8u, (uint32_t)g.col_tiles - group * 8);
@@ -235,8 +241,8 @@ __global__ __launch_bounds__(64 * WM * WN) void ffn_product_kernel(ProductArgs g
   const int M = kKind == kDwOut ? D : kKind == kDwIn ? 2 * F : n;
   const int n0 = tn * kCols;
 
-  Loader<T, kAcrossA, kFast, BM, kThreads> la;
-  Loader<T, kAcrossB, kFast, BN, kThreads> lb;
+  Loader<T, kAcrossA, kMapped && kKind == kDwOut, kFast, BM, kBytes, kThreads> la;
+  Loader<T, kAcrossB, kMapped && kKind == kDwIn, kFast, BN, kBytes, kThreads> lb;
   if constexpr (kAcrossA) la.across(oa, K, t.row, M);
   else la.along(oa, K, [&](int r) { return min(t.row + r, M - 1); });
   if constexpr (kAcrossB) {
@@ -259,108 +265,248 @@ __global__ __launch_bounds__(64 * WM * WN) void ffn_product_kernel(ProductArgs g
 #pragma unroll
     for (int j = 0; j < NI; j++) acc[i][j] = F4{0, 0, 0, 0};
 
-  const int steps = (K + kStepK<T> - 1) / kStepK<T>;
-  if (steps > 0) {
-    la.load(0, lds);
-    lb.load(0, lds + BM * kStepBytes);
-    la.store(lds);
-    lb.store(lds + BM * kStepBytes);
-  }
-  for (int s = 0; s < steps; s++) {
-    char *now = lds + (s & 1) * kBuffer, *next = lds + (~s & 1) * kBuffer;
-    tile_barrier();
-    if (s + 1 < steps) {
-      la.load((s + 1) * kStepK<T>, next);
-      lb.load((s + 1) * kStepK<T>, next + BM * kStepBytes);
-    }
+  constexpr int kStep = kBytes / (int)sizeof(T);
+  const int steps = (K + kStep - 1) / kStep;
+  constexpr int kLoads = la.kLoads + lb.kLoads;
+  const int turn = (int)((uint64_t)steps * (id >> 3 & 31) / 32);
+  auto place = [&](int s) {  // in the shared axis, of step s
+    return (s >= steps ? s : s + turn >= steps ? s + turn - steps : s + turn) * kStep;
+  };
+  // A step's products, row of parts by row, whose operands are read two rows
+  // ahead; `ahead(q)` is called before row q. The order is kept as it stands:
+  // by itself the compiler reads an operand right where it is needed.
+  auto multiply_step = [&](const char *from, auto ahead) {
+    constexpr int kHalves = kBytes / 64, kDepth = MI < 2 ? 1 : 2;
+    Frag<T> fa[kHalves][MI], fb[kHalves][NI];
+    auto read_a = [&](int q) {
+      fa[q / MI][q % MI] = read_frag<T, kAcrossA, BM, kBytes>(from, wm + 16 * (q % MI), q / MI);
+    };
+    auto read_b = [&](int h, int j) {
+      fb[h][j] = read_frag<T, kAcrossB, BN, kBytes>(from + kTileA, wn + 16 * j, h);
+    };
 #pragma unroll
-    for (int h = 0; h < 2; h++) {
-      Frag<T> fa[MI], fb[NI];
+    for (int j = 0; j < NI; j++) read_b(0, j);
 #pragma unroll
-      for (int i = 0; i < MI; i++) fa[i] = read_frag<T, kAcrossA, BM>(now, wm + 16 * i, h);
+    for (int q = 0; q < kDepth; q++) read_a(q);
+#pragma unroll
+    for (int q = 0; q < kHalves * MI; q++) {
+      if (q + kDepth < kHalves * MI) read_a(q + kDepth);
+      if (q / MI + 1 < kHalves && q % MI >= MI - kDepth) {
+#pragma unroll
+        for (int j = 0; j < NI / kDepth; j++)
+          read_b(q / MI + 1, (q % MI - (MI - kDepth)) * (NI / kDepth) + j);
+      }
+      ahead(q);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int j = 0; j < NI; j++)
-        fb[j] = read_frag<T, kAcrossB, BN>(now + BM * kStepBytes, wn + 16 * j, h);
-#pragma unroll
-      for (int i = 0; i < MI; i++)
-#pragma unroll
-        for (int j = 0; j < NI; j++) acc[i][j] = multiply(fb[j], fa[i], acc[i][j]);
+        acc[q % MI][j] = multiply(fb[q / MI][j], fa[q / MI][q % MI], acc[q % MI][j]);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (s + 1 < steps) {
-      la.store(next);
-      lb.store(next + BM * kStepBytes);
+  };
+  if constexpr (kFast) {
+    // Every step loads, past the end zeros that nothing uses, so that a step's
+    // loads are there when no more than those of S - 2 steps are on their way.
+    auto load = [&](int i, int s, char *to) {
+      if (i < la.kLoads) la.load(i, place(s), to);
+      else lb.load(i - la.kLoads, place(s), to + kTileA);
+    };
+#pragma unroll
+    for (int s = 0; s < S - 1; s++)
+#pragma unroll
+      for (int i = 0; i < kLoads; i++) load(i, s, lds + s * kBuffer);
+    int now = 0;
+    for (int s = 0; s < steps; s++) {
+      tile_barrier<kLoads *(S - 2)>();
+      char *next = lds + (now == 0 ? S - 1 : now - 1) * kBuffer;
+      multiply_step(lds + now * kBuffer, [&](int q) {
+#pragma unroll
+        for (int i = 0; i < kLoads; i++)
+          if (i >= q * kLoads / MI && i < (q + 1) * kLoads / MI) load(i, s + S - 1, next);
+      });
+      now = now == S - 1 ? 0 : now + 1;
+    }
+  } else {
+    // chunks wait in registers, those of two steps on their way
+    Chunk held[2][kLoads];
+    auto fetch = [&](Chunk(&h)[kLoads], int s) {
+      const int k0 = place(s);
+      if (la.whole(k0) && lb.whole(k0)) {
+#pragma unroll
+        for (int i = 0; i < kLoads; i++)
+          h[i] = i < la.kLoads ? la.fetch(i, k0, true) : lb.fetch(i - la.kLoads, k0, true);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kLoads; i++)
+          h[i] = i < la.kLoads ? la.fetch(i, k0, false) : lb.fetch(i - la.kLoads, k0, false);
+      }
+    };
+    auto keep = [&](const Chunk(&h)[kLoads], char *to) {  // B's chunks lie behind A's
+#pragma unroll
+      for (int i = 0; i < kLoads; i++) *(Chunk *)(to + (i * kThreads + threadIdx.x) * 16) = h[i];
+    };
+    fetch(held[0], 0);
+    fetch(held[1], 1);
+    keep(held[0], lds);
+    auto step = [&](int s, Chunk(&old)[kLoads], Chunk(&later)[kLoads]) {
+      tile_barrier<63>();  // of LDS alone
+      fetch(old, s + 2);
+      multiply_step(lds + (s & 1) * kBuffer, [](int) {});
+      keep(later, lds + (~s & 1) * kBuffer);
+    };
+    for (int s = 0; s < steps; s += 2) {
+      step(s, held[0], held[1]);
+      if (s + 1 < steps) step(s + 1, held[1], held[0]);
     }
   }
 
   // Lane l has columns l / 16 * 4 + 0..3 of row l % 16 of every 16 x 16 part.
+  // Each wavefront passes 16 rows at a time through LDS of its own, so that a
+  // row's results leave in whole chunks next to each other (stored as they are,
+  // 8 bytes here and there, the weights' gradient took three times as long).
+  tile_barrier<0>();
+  constexpr int kN = Vec<T>::kN, kPitch = 16 * NI * 4 + 16;
+  constexpr int kPer = (kKind == kUp ? 8 : 16) * NI / kN;  // chunks of a row
+  char *own = lds + wave * (16 * kPitch);
 #pragma unroll
   for (int i = 0; i < MI; i++) {
-    const int m = t.row + wm + 16 * i + (lane & 15);
-    if (m >= M) continue;
-    const int64_t compact = first + m, row = kWeights ? 0 : map ? map[m] : compact;
-    const int c0 = lane >> 4 << 2;
-    if constexpr (kKind == kUp) {
 #pragma unroll
-      for (int j = 0; j < NI / 2; j++) {
-        const int f = n0 + wn / 2 + 16 * j + c0, left = F - f;
-        const F4 gate = acc[i][j], up = acc[i][j + NI / 2];
-        F4 a;
+    for (int j = 0; j < NI; j++)
+      *(F4 *)(own + (lane & 15) * kPitch + (16 * j + (lane >> 4) * 4) * 4) = acc[i][j];
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-        for (int x = 0; x < 4; x++) a[x] = gate[x] * sigmoid<T>(gate[x]) * up[x];
-        store_four<T, kFast>((T *)g.out + compact * F + f, a, left);
+    for (int it = 0; it < (16 * kPer + 63) / 64; it++) {
+      const int id = it * 64 + lane, r = id / kPer, c = id % kPer * kN;
+      const int m = t.row + wm + 16 * i + r;
+      if (r >= 16 || m >= M) continue;
+      const char *from = own + r * kPitch + c * 4;
+      const int64_t compact = first + m, row = kWeights ? 0 : map ? map[m] : compact;
+      if constexpr (kKind == kUp) {
+        const int f = n0 + wn / 2 + c, left = F - f;
+        typename Vec<T>::V a, gate, up;
+#pragma unroll
+        for (int x = 0; x < kN; x++) {
+          const float vg = *(const float *)(from + 4 * x);
+          const float vu = *(const float *)(from + 32 * NI + 4 * x);
+          gate[x] = (T)vg;
+          up[x] = (T)vu;
+          a[x] = (T)(vg * sigmoid<T>(vg) * vu);
+        }
+        store_vec<T, !kFast>((T *)g.out + compact * F + f, a, left);
         if (g.more) {
           T *pre = (T *)g.more + row * 2 * F + f;
-          store_four<T, kFast>(pre, gate, left);
-          store_four<T, kFast>(pre + F, up, left);
+          store_vec<T, !kFast>(pre, gate, left);
+          store_vec<T, !kFast>(pre + F, up, left);
         }
-      }
-    } else if constexpr (kKind == kGrad) {
-#pragma unroll
-      for (int j = 0; j < NI; j++) {
-        const int f = n0 + wn + 16 * j + c0, left = F - f;
+      } else if constexpr (kKind == kGrad) {
+        const int f = n0 + wn + c, left = F - f;
         const T *pre = (const T *)g.pre + row * 2 * F + f;
-        const F4 gate = load_four<T, kFast>(pre, left), up = load_four<T, kFast>(pre + F, left);
-        F4 a, dg, du;
+        const auto gate = load_vec<T, !kFast>(pre, left), up = load_vec<T, !kFast>(pre + F, left);
+        typename Vec<T>::V a, dg, du;
 #pragma unroll
-        for (int x = 0; x < 4; x++) {
-          const float sg = sigmoid<T>(gate[x]), da = acc[i][j][x], act = gate[x] * sg;
-          a[x] = act * up[x];
-          du[x] = da * act;
-          dg[x] = da * up[x] * (sg * (1.0f + gate[x] * (1.0f - sg)));
+        for (int x = 0; x < kN; x++) {
+          const float vg = (float)gate[x], vu = (float)up[x], sg = sigmoid<T>(vg), act = vg * sg;
+          const float da = *(const float *)(from + 4 * x);
+          a[x] = (T)(act * vu);
+          du[x] = (T)(da * act);
+          dg[x] = (T)(da * vu * (sg * (1.0f + vg * (1.0f - sg))));
         }
         T *dpre = (T *)g.out + compact * 2 * F + f;
-        store_four<T, kFast>(dpre, dg, left);
-        store_four<T, kFast>(dpre + F, du, left);
-        store_four<T, kFast>((T *)g.more + compact * F + f, a, left);
-      }
-    } else {
-      const int64_t to = kKind == kDwOut ? (int64_t)e * D + m : kKind == kDwIn ? (int64_t)e * 2 * F + m : row;
+        store_vec<T, !kFast>(dpre, dg, left);
+        store_vec<T, !kFast>(dpre + F, du, left);
+        store_vec<T, !kFast>((T *)g.more + compact * F + f, a, left);
+      } else {
+        const int64_t to = kKind == kDwOut  ? (int64_t)e * D + m
+                           : kKind == kDwIn ? (int64_t)e * 2 * F + m
+                                            : row;
+        typename Vec<T>::V v;
 #pragma unroll
-      for (int j = 0; j < NI; j++) {
-        const int c = n0 + wn + 16 * j + c0;
-        store_four<T, kFast>((T *)g.out + to * N + c, acc[i][j], N - c);
+        for (int x = 0; x < kN; x++) v[x] = (T)*(const float *)(from + 4 * x);
+        store_vec<T, !kFast>((T *)g.out + to * N + n0 + wn + c, v, N - (n0 + wn + c));
       }
     }
+    // the next rows' writes stay behind these reads
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 }
 
-// a tile's shape
-struct Shape {
-  int rows, cols, threads;
-};
-constexpr Shape kLarge{256, 256, 512}, kSmall{128, 128, 256};
+using Tiny = Shape<32, 64, 2, 2, 128, 4>;
+using Small = Shape<64, 64, 2, 2, 128, 2>;
+using Medium = Shape<128, 128, 2, 2, 128, 2>;
+using Wide = Shape<128, 256, 2, 4, 128, 3>;
+using Large = Shape<256, 256, 2, 4, 128, 2>;
+using Deep = Shape<256, 256, 2, 4, 64, 5>;
+enum Size { kTiny, kSmall, kMedium, kWide, kLarge };
 
-template <class T, int kKind, bool kFast>
-const void *product_fn(bool large) {
-  if constexpr (kFast && sizeof(T) == 2)
-    if (large) return (const void *)ffn_product_kernel<T, kKind, kFast, 256, 256, 2, 4>;
-  return (const void *)ffn_product_kernel<T, kKind, kFast, 128, 128, 2, 2>;
+template <class T, int kKind, bool kMapped, bool kFast, class Z>
+__global__ __launch_bounds__(Z::kThreads, Z::BM == 64 ? 4 : 2) void ffn_product_kernel(ProductArgs g) {
+  extern __shared__ __align__(16) char lds[];
+  product<T, kKind, kMapped, kFast, Z>(g, blockIdx.x, lds);
+}
+
+// The three products of the gradient that need dg and du (and a), in one launch:
+// blocks up to dx's, those of w_in's gradient, and the rest.
+struct LastArgs {
+  ProductArgs dx, in, out;
+  uint32_t dx_blocks, in_blocks;
+};
+template <class T, bool kMapped, bool kFast, class Z>
+__global__ __launch_bounds__(Z::kThreads, Z::BM == 64 ? 4 : 2) void ffn_last_kernel(LastArgs g) {
+  extern __shared__ __align__(16) char lds[];
+  uint32_t b = blockIdx.x;
+  if (b < g.dx_blocks) return product<T, kDx, false, kFast, Z>(g.dx, b, lds);
+  b -= g.dx_blocks;
+  if (b < g.in_blocks) return product<T, kDwIn, kMapped, kFast, Z>(g.in, b, lds);
+  product<T, kDwOut, kMapped, kFast, Z>(g.out, b - g.in_blocks, lds);
+}
+
+// What a launch needs to know of a kernel
+struct Kernel {
+  const void *fn;
+  int rows, cols, threads, lds;
+};
+template <class Z>
+Kernel shaped(const void *fn) {
+  return {fn, Z::BM, Z::BN, Z::kThreads, Z::kLds};
+}
+template <class T, int kKind, bool kMapped, bool kFast>
+Kernel kernel_of(Size size) {
+#define F(Z) shaped<Z>((const void *)ffn_product_kernel<T, kKind, kMapped, kFast, Z>)
+  if constexpr (kKind == kDwOut || kKind == kDwIn) {  // smaller ones: ffn_last_kernel
+    if constexpr (kFast && sizeof(T) == 2) return size == kWide ? F(Wide) : F(Deep);
+  } else {
+    if constexpr (kFast && sizeof(T) == 2) {
+      if (size == kWide) return F(Wide);
+      if (size == kLarge) return F(Large);
+    }
+    return size == kTiny ? F(Tiny) : size == kSmall ? F(Small) : F(Medium);
+  }
+#undef F
+}
+template <class T, int kKind>
+Kernel kernel_of(bool mapped, bool fast, Size size) {
+  if constexpr (kKind == kDwOut || kKind == kDwIn)  // the others' rows are fixed before the steps
+    return mapped ? kernel_of<T, kKind, true, true>(size) : kernel_of<T, kKind, false, true>(size);
+  else
+    return fast ? kernel_of<T, kKind, false, true>(size) : kernel_of<T, kKind, false, false>(size);
 }
 template <int kKind>
-const void *product_of(int dtype, bool fast, bool large) {
-#define F(T) (fast ? product_fn<T, kKind, true>(large) : product_fn<T, kKind, false>(large))
-  return dtype == TACCL_F32 ? F(float) : dtype == TACCL_BF16 ? F(bf16_t) : F(f16_t);
+Kernel kernel_of(int dtype, bool mapped, bool fast, Size size) {
+  if constexpr (kKind != kDwOut && kKind != kDwIn)
+    if (dtype == TACCL_F32) return kernel_of<float, kKind>(mapped, fast, size);
+  return dtype == TACCL_BF16 ? kernel_of<bf16_t, kKind>(mapped, fast, size)
+                             : kernel_of<f16_t, kKind>(mapped, fast, size);
+}
+template <class T, bool kMapped, bool kFast>
+Kernel last_kernel(Size size) {
+#define F(Z) shaped<Z>((const void *)ffn_last_kernel<T, kMapped, kFast, Z>)
+  return size == kSmall ? F(Small) : F(Medium);
 #undef F
+}
+template <class T>
+Kernel last_kernel(bool mapped, bool fast, Size size) {
+  return mapped ? (fast ? last_kernel<T, true, true>(size) : last_kernel<T, true, false>(size))
+                : (fast ? last_kernel<T, false, true>(size) : last_kernel<T, false, false>(size));
 }
 
 template <class... P>
@@ -371,77 +517,109 @@ bool aligned16(P... p) {
 // What the launches of a call share
 struct Products {
   ProductArgs base{};
-  Shape shape;
-  bool fast, large;
-  int dtype;
+  const FfnTile *tiles[kLists];
+  bool fast;
+  int dtype, cus;
   int64_t slots;
   hipStream_t stream;
 
-  // kKind's launch; `m`: rows of the weights' gradient, else 0; n: columns
+  int64_t count(int64_t m, int64_t n, int rows, int cols) const {
+    return base.experts * ((m + rows - 1) / rows) * ((n + cols - 1) / cols);
+  }
+  // Size of the tiles of a product of m rows and n columns per expert
+  Size size_of(int64_t m, int64_t n) const {
+    if (fast && dtype != TACCL_F32) {
+      if (count(m, n, 256, 256) >= 4 * cus) return kLarge;
+      if (4 * count(m, n, 128, 256) >= 3 * cus) return kWide;
+    }
+    if (2 * count(m, n, 128, 128) >= 3 * cus) return kMedium;
+    return count(m, n, 64, 64) >= cus ? kSmall : kTiny;
+  }
+
+  // the list that a product's kernel reads, as a bit
   template <int kKind>
-  hipError_t run(const void *a, const void *b, void *out, int m, int n, void *more = nullptr,
-                 const void *pre = nullptr) const {
+  int list(int64_t m, int64_t n) const {
+    const Kernel k = kernel_of<kKind>(dtype, base.map != nullptr, fast, size_of(m, n));
+    return 1 << list_of(k.rows);
+  }
+  // arguments of a product with this kernel's tiles, and its blocks
+  template <int kKind>
+  ProductArgs args(const Kernel &k, const void *a, const void *b, void *out, int64_t m, int64_t n,
+                   uint32_t &blocks) const {
     ProductArgs g = base;
     g.a = a;
     g.b = b;
     g.out = out;
+    g.tiles = tiles[list_of(k.rows)];
+    g.num_tiles += list_of(k.rows);
+    g.col_tiles = (int)((n + k.cols - 1) / k.cols);
+    g.row_tiles = (int)((m + k.rows - 1) / k.rows);
+    // ids come in pieces of 32 by 8 XCDs
+    blocks = out ? (uint32_t)(((int64_t)g.experts * g.row_tiles * g.col_tiles + 255) / 256 * 256) : 0;
+    return g;
+  }
+  // a product of m rows and n columns per expert
+  template <int kKind>
+  hipError_t run(const void *a, const void *b, void *out, int64_t m, int64_t n,
+                 void *more = nullptr, const void *pre = nullptr) const {
+    const Kernel k = kernel_of<kKind>(dtype, base.map != nullptr, fast, size_of(m, n));
+    uint32_t blocks;
+    ProductArgs g = args<kKind>(k, a, b, out, m, n, blocks);
     g.more = more;
     g.pre = pre;
-    const int per = kKind == kUp ? shape.cols / 2 : shape.cols;
-    g.col_tiles = (n + per - 1) / per;
-    g.row_tiles = (m + shape.rows - 1) / shape.rows;
-    const int64_t entries = g.experts * (m ? g.row_tiles : (slots + shape.rows - 1) / shape.rows);
-    // ids come in pieces of 32 by 8 XCDs
-    const int64_t blocks = (entries * g.col_tiles + 255) / 256 * 256;
-    const uint32_t bytes = 2 * (shape.rows + shape.cols) * kStepBytes;
-    void *args[] = {&g};
-    return hipLaunchKernel(product_of<kKind>(dtype, fast, large), dim3((uint32_t)blocks),
-                           dim3(shape.threads), args, bytes, stream);
+    void *p[] = {&g};
+    if (!out) return hipSuccess;
+    return hipLaunchKernel(k.fn, dim3(blocks), dim3(k.threads), p, k.lds, stream);
   }
 };
 
 template <class A>
-hipError_t prepare(const A &a, const FfnSpace &sp, bool fast, int cus, void *zero,
-                   hipStream_t stream, Products &p) {
+Products products(const A &a, const FfnSpace &sp, bool fast, int cus, hipStream_t stream) {
   uint8_t *ws = (uint8_t *)a.workspace;
-  const int64_t size = a.dtype == TACCL_F32 ? 4 : 2;
+  Products p;
   p.dtype = a.dtype;
   p.fast = fast;
+  p.cus = cus;
   p.slots = a.sources * a.capacity;
   p.stream = stream;
-  // the large tile where it leaves every CU two tiles of the smaller product
-  const int64_t tiles = a.num_experts * ((p.slots + 255) / 256) *
-                        ((std::min(a.cols, 2 * a.hidden) + 255) / 256);
-  p.large = fast && size == 2 && tiles >= 2 * cus;
-  p.shape = p.large ? kLarge : kSmall;
   ProductArgs &g = p.base;
   g.rows = (const int32_t *)(ws + sp.rows);
   g.num_tiles = (const int32_t *)(ws + sp.num_tiles);
-  g.tiles = (const FfnTile *)(ws + sp.tiles);
   g.map = a.sources > 1 ? (const int32_t *)(ws + sp.map) : nullptr;
   g.slots = p.slots;
   g.cols = a.cols;
   g.hidden = a.hidden;
   g.experts = a.num_experts;
+  for (int i = 0; i < kLists; i++) p.tiles[i] = (const FfnTile *)(ws + sp.tiles[i]);
+  return p;
+}
+
+// The first launch, for products with tiles of the lists `lists`
+template <class A>
+hipError_t launch_plan(const A &a, const Products &p, int lists, void *zero) {
   PlanArgs q{};
   q.counts = a.counts;
   q.capacity = a.capacity;
   q.sources = a.sources;
   q.experts = a.num_experts;
-  q.tile = p.shape.rows;
-  q.parts = zero || g.map ? (int)std::max<int64_t>(1, std::min<int64_t>(
-                                p.slots, (4 * (int64_t)cus + q.experts - 1) / q.experts))
-                          : 0;
-  q.rows = (int32_t *)(ws + sp.rows);
-  q.num_tiles = (int32_t *)(ws + sp.num_tiles);
-  q.map = (int32_t *)g.map;
-  q.tiles = (FfnTile *)(ws + sp.tiles);
+  q.rows = (int32_t *)p.base.rows;
+  q.num_tiles = (int32_t *)p.base.num_tiles;
+  q.map = (int32_t *)p.base.map;
+  for (int i = 0; i < kLists; i++) q.tiles[i] = (FfnTile *)p.tiles[i];
+  q.lists = lists;
   q.zero = (uint8_t *)zero;
-  q.row_bytes = a.cols * size;
+  q.row_bytes = a.cols * (a.dtype == TACCL_F32 ? 4 : 2);
+  // four blocks per CU, in whole ones per piece
+  auto parts = [&](int64_t pieces, int64_t most) {
+    return (int)std::max<int64_t>(1, std::min(most, (4 * p.cus + pieces - 1) / pieces));
+  };
+  const int64_t pieces = (int64_t)q.sources * q.experts;
+  if (q.map) q.map_parts = parts(q.experts, (p.slots + kPlanThreads - 1) / kPlanThreads);
+  if (zero) q.zero_parts = parts(pieces, q.capacity);
+  const int64_t blocks = 1 + (int64_t)q.experts * q.map_parts + pieces * q.zero_parts;
   void *args[] = {&q};
-  return hipLaunchKernel((const void *)ffn_plan_kernel,
-                         dim3(1 + (uint32_t)q.experts * (uint32_t)q.parts), dim3(kPlanThreads),
-                         args, 0, stream);
+  return hipLaunchKernel((const void *)ffn_plan_kernel, dim3((uint32_t)blocks), dim3(kPlanThreads),
+                         args, 0, p.stream);
 }
 
 // whole, aligned chunks everywhere
@@ -457,11 +635,12 @@ hipError_t launch_ffn(const taccl_ffn_t &a, int cus, hipStream_t stream) {
       ffn_space(a.sources, a.num_experts, a.capacity, a.hidden, a.dtype, false);
   const bool fast = whole_chunks(a.dtype, a.cols, a.hidden) &&
                     aligned16(a.buffer, a.w_in, a.w_out, a.out, a.pre);
-  Products p;
-  hipError_t e = prepare(a, sp, fast, cus, a.out, stream, p);
+  const Products p = products(a, sp, fast, cus, stream);
   void *act = (uint8_t *)a.workspace + sp.act;
-  if (e == hipSuccess) e = p.run<kUp>(a.buffer, a.w_in, act, 0, a.hidden, a.pre);
-  if (e == hipSuccess) e = p.run<kDown>(act, a.w_out, a.out, 0, a.cols);
+  const int64_t D = a.cols, F = a.hidden;
+  hipError_t e = launch_plan(a, p, p.list<kUp>(p.slots, 2 * F) | p.list<kDown>(p.slots, D), a.out);
+  if (e == hipSuccess) e = p.run<kUp>(a.buffer, a.w_in, act, p.slots, 2 * F, a.pre);
+  if (e == hipSuccess) e = p.run<kDown>(act, a.w_out, a.out, p.slots, D);
   return e;
 }
 
@@ -470,14 +649,39 @@ hipError_t launch_ffn_backward(const taccl_ffn_backward_t &a, int cus, hipStream
   const bool fast =
       whole_chunks(a.dtype, a.cols, a.hidden) &&
       aligned16(a.dout, a.buffer, a.w_in, a.w_out, a.pre, a.dbuffer, a.dw_in, a.dw_out);
-  Products p;
-  hipError_t e = prepare(a, sp, fast, cus, a.dbuffer, stream, p);
+  const Products p = products(a, sp, fast, cus, stream);
   void *act = (uint8_t *)a.workspace + sp.act, *dpre = (uint8_t *)a.workspace + sp.dpre;
-  if (e == hipSuccess) e = p.run<kGrad>(a.dout, a.w_out, dpre, 0, a.hidden, act, a.pre);
-  if (e == hipSuccess && a.dbuffer) e = p.run<kDx>(dpre, a.w_in, a.dbuffer, 0, a.cols);
-  if (e == hipSuccess && a.dw_out) e = p.run<kDwOut>(a.dout, act, a.dw_out, a.cols, a.hidden);
-  if (e == hipSuccess && a.dw_in) e = p.run<kDwIn>(dpre, a.buffer, a.dw_in, 2 * a.hidden, a.cols);
-  return e;
+  const int64_t D = a.cols, F = a.hidden;
+  const bool mapped = p.base.map != nullptr;
+  // Large products one by one, small ones together: alone they leave CUs empty.
+  const bool each = fast && a.dtype != TACCL_F32 &&
+                    std::min({p.size_of(p.slots, D), p.size_of(2 * F, D), p.size_of(D, F)}) >= kWide;
+  const int64_t tiles = p.count(p.slots, D, 128, 128) + p.count(2 * F, D, 128, 128) +
+                        p.count(D, F, 128, 128);
+  const Size size = tiles >= 8 * cus ? kMedium : kSmall;
+  const Kernel k = a.dtype == TACCL_F32    ? last_kernel<float>(mapped, fast, size)
+                   : a.dtype == TACCL_BF16 ? last_kernel<bf16_t>(mapped, fast, size)
+                                           : last_kernel<f16_t>(mapped, fast, size);
+  hipError_t e = launch_plan(a, p,
+                             p.list<kGrad>(p.slots, F) |
+                                 (each ? p.list<kDx>(p.slots, D) : 1 << list_of(k.rows)),
+                             a.dbuffer);
+  if (e == hipSuccess) e = p.run<kGrad>(a.dout, a.w_out, dpre, p.slots, F, act, a.pre);
+  if (e != hipSuccess) return e;
+  if (each) {
+    e = p.run<kDx>(dpre, a.w_in, a.dbuffer, p.slots, D);
+    if (e == hipSuccess) e = p.run<kDwIn>(dpre, a.buffer, a.dw_in, 2 * F, D);
+    if (e == hipSuccess) e = p.run<kDwOut>(a.dout, act, a.dw_out, D, F);
+    return e;
+  }
+  LastArgs g{};
+  uint32_t out_blocks;
+  g.dx = p.args<kDx>(k, dpre, a.w_in, a.dbuffer, p.slots, D, g.dx_blocks);
+  g.in = p.args<kDwIn>(k, dpre, a.buffer, a.dw_in, 2 * F, D, g.in_blocks);
+  g.out = p.args<kDwOut>(k, a.dout, act, a.dw_out, D, F, out_blocks);
+  void *args[] = {&g};
+  return hipLaunchKernel(k.fn, dim3(g.dx_blocks + g.in_blocks + out_blocks), dim3(k.threads), args,
+                         k.lds, stream);
 }
 
 }  // namespace taccl

@@ -1,12 +1,12 @@
 // Matrix products on tiles in LDS for the experts' feed-forward (gfx950).
 //
 // A block multiplies BM rows of one operand by BN rows of the other over steps
-// of 128 bytes of the shared axis (kStepK elements). Either operand is stored
-// with the shared axis contiguous ("along") or as rows of it ("across"); its
-// tile lies in LDS the way it is stored, in 16-byte chunks whose order within a
-// row is permuted so that the reads of a matrix instruction's operand touch
-// every bank equally often. Loads go straight to LDS where every chunk is
-// aligned and whole (kFast), else through registers.
+// of 64 or 128 bytes of the shared axis. Either operand is stored with the
+// shared axis contiguous ("along") or as rows of it ("across"); its tile lies
+// in LDS the way it is stored, in 16-byte chunks whose order within a row is
+// permuted so that the reads of a matrix instruction's operand touch every bank
+// equally often. Where every chunk is aligned and whole (kFast), loads go
+// straight to LDS, several steps ahead; else through registers, one ahead.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -21,13 +21,25 @@ typedef uint32_t Chunk __attribute__((ext_vector_type(4)));
 // what lanes past the shared axis' end load; never written
 static __device__ Chunk zero_chunk;
 
-__device__ __forceinline__ void load_to_lds(const void *p, void *lds) {
-  __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void *)p,
-                                   (__attribute__((address_space(3))) void *)lds, 16, 0, 0);
+// 16 bytes per lane from p to LDS, the wavefront's from `lds` on. As a builtin
+// the compiler waits for all such loads before every transposing read, which
+// it takes to read what they write; so it does not see them, and whoever reads
+// their LDS waits for them itself (tile_barrier). There is no register that they
+// write.
+__device__ __forceinline__ void load_to_lds(const void *p, char *lds) {
+  const uint32_t at = __builtin_amdgcn_readfirstlane(
+      (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds);
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               :
+               : "v"(p), "s"(at)
+               : "memory");
 }
-// all of the block's loads to LDS are there, and all its reads of LDS are done
+// All but the newest kLater of the wavefront's loads are there and its reads of
+// LDS are done, and the same holds for the block's other wavefronts.
+template <int kLater>
 __device__ __forceinline__ void tile_barrier() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  static_assert(kLater < 64);
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLater) : "memory");
 }
 
 // One operand's part of a step: 16 rows by 64 bytes of the shared axis, a chunk
@@ -50,9 +62,8 @@ __device__ __forceinline__ F4 multiply(const Frag<float> &a, const Frag<float> &
   return c;
 }
 
-// An operand in memory: `rows` rows (tile rows where the shared axis is along
-// them, else rows of that axis), `ld` elements apart from `p`, or where `map`
-// says.
+// An operand in memory: rows (tile rows where the shared axis is along them,
+// else rows of that axis) `ld` elements apart from `p`, or where `map` says.
 template <class T>
 struct Operand {
   const T *p;
@@ -63,40 +74,37 @@ struct Operand {
   }
 };
 
-constexpr int kStepBytes = 128;
-template <class T>
-constexpr int kStepK = kStepBytes / (int)sizeof(T);
-
-// The place of chunk `c` in row r of a tile across the shared axis, whose rows
-// have kChunks chunks. A 16-bit operand is read 32 bytes (two chunks) from each
-// of the rows 8 g + 0..3 (g < 4), a 32-bit one 64 bytes from each of 4 g + i.
-template <class T, int kChunks>
-__device__ __forceinline__ int across_place(int r, int c) {
+// The place of chunk `c` in row r of a tile whose rows have kChunks chunks.
+// Along: sixteen rows' chunks of one number are read at a time, eight of them
+// in each pass over the banks. Across: a 16-bit operand is read 32 bytes (two
+// chunks) from each of the rows 8 g + 0..3 (g < 4), a 32-bit one 64 bytes from
+// each of 4 g + i.
+template <class T, bool kAcross, int kChunks>
+__device__ __forceinline__ int chunk_place(int r, int c) {
+  if (!kAcross) return c ^ (kChunks == 8 ? r & 7 : r >> 1 & 3);
   if (sizeof(T) == 2) return c ^ ((((r & 3) | (r >> 3 & 3) << 2) << 1) & (kChunks - 1));
   return c ^ (((r >> 2 & 3) << 2) & (kChunks - 1));
 }
 
 // The loads of an operand's tile of kRows rows (columns where the shared axis
-// is across) by a block of kThreads threads.
-template <class T, bool kAcross, bool kFast, int kRows, int kThreads>
+// is across) over kBytes bytes of the shared axis, by kThreads threads.
+template <class T, bool kAcross, bool kMapped, bool kFast, int kRows, int kBytes, int kThreads>
 struct Loader {
-  static constexpr int kLoads = kRows * 8 / kThreads;
-  static constexpr int kN = Vec<T>::kN;
-  static constexpr int kChunks = kAcross ? kRows / kN : 8;  // per row in LDS
-  static_assert(kRows * 8 % kThreads == 0);
+  static constexpr int kLoads = kRows * kBytes / 16 / kThreads;
+  static constexpr int kN = Vec<T>::kN, kStep = kBytes / (int)sizeof(T);
+  static constexpr int kChunks = kAcross ? kRows / kN : kBytes / 16;  // per row in LDS
+  static_assert(kRows * kBytes / 16 % kThreads == 0);
 
   Operand<T> o;
-  const T *at[kLoads];  // along: the row's next chunk
+  const T *at[kLoads];  // the chunk of the first step
   int K;                // the shared axis' length
   int col, cols;        // across: the tile's first column and their number
-  Chunk held[kFast ? 1 : kLoads];
 
   static __device__ __forceinline__ int chunk_id(int i) { return i * kThreads + threadIdx.x; }
   // row of load i in LDS and the chunk of the operand that belongs there
   static __device__ __forceinline__ int row(int i) { return chunk_id(i) / kChunks; }
   static __device__ __forceinline__ int source(int i) {
-    const int c = chunk_id(i) % kChunks, r = row(i);
-    return kAcross ? across_place<T, kChunks>(r, c) : c ^ (r & 7);
+    return chunk_place<T, kAcross, kChunks>(row(i), chunk_id(i) % kChunks);
   }
 
   // tile row r is row `from(r)` of the operand
@@ -113,10 +121,9 @@ struct Loader {
     K = k;
     col = c;
     cols = n;
-    if (!o.map) {
 #pragma unroll
-      for (int i = 0; i < kLoads; i++) at[i] = o.p + (int64_t)row(i) * o.ld + column(i);
-    }
+    for (int i = 0; i < kLoads; i++)
+      at[i] = o.p + (kMapped ? 0 : (int64_t)row(i) * o.ld) + column(i);
   }
   // a chunk past the last column takes the tile's first one: its results are
   // not stored
@@ -124,52 +131,64 @@ struct Loader {
     const int c = col + source(i) * kN;
     return c < cols ? c : col;
   }
-
-  // Step k0 of the tile, to `lds` (kFast) or on its way to `held`.
-  __device__ __forceinline__ void load(int k0, char *lds) {
-    const bool last = k0 + kStepK<T> > K;
+  // The map's entry for row k of load i. A wavefront's load has few rows, whose
+  // entries are scalar loads: vector loads would be waited for behind all tiles
+  // on their way.
+  __device__ __forceinline__ int64_t mapped(int i, int k0) const {
+    constexpr int kPer = kChunks >= 64 ? 1 : 64 / kChunks;
+    typedef const __attribute__((address_space(4))) int32_t *Scalar;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int first = k0 + (i * kThreads + wave * 64) / kChunks;
+    const int mine = (threadIdx.x & 63) / kChunks;
+    int32_t at = 0;
 #pragma unroll
-    for (int i = 0; i < kLoads; i++) {
-      const T *p;
-      int left;  // elements of the chunk that exist
-      if (kAcross) {
-        const int r = k0 + row(i);
-        if (o.map) {
-          p = r < K ? o.row(r) + column(i) : nullptr;
-        } else {
-          p = at[i];
-          at[i] += kStepK<T> * o.ld;
-        }
-        left = !last || r < K ? (kFast ? kN : min(cols - column(i), kN)) : 0;
-      } else {
-        p = at[i];
-        at[i] += kStepK<T>;
-        left = last ? K - k0 - source(i) * kN : kN;
-      }
-      if (kFast) {
-        if (last && left <= 0) p = (const T *)&zero_chunk;
-        load_to_lds(p, lds + (i * kThreads + (threadIdx.x & ~63)) * 16);
-      } else {
-        held[i] = __builtin_bit_cast(Chunk, load_vec<T, true>(p, left));
-      }
+    for (int j = 0; j < kPer; j++) {
+      const int32_t v = ((Scalar)(uintptr_t)o.map)[max(min(first + j, K - 1), 0)];
+      at = mine == j ? v : at;
     }
+    return at;
   }
-  __device__ __forceinline__ void store(char *lds) const {
-    if (kFast) return;
-#pragma unroll
-    for (int i = 0; i < kLoads; i++) *(Chunk *)(lds + chunk_id(i) * 16) = held[i];
+
+  // Chunk i of the step from k0 on; `left` elements of it exist
+  __device__ __forceinline__ const T *chunk(int i, int k0, int &left) const {
+    const bool last = k0 + kStep > K;
+    left = kN;
+    if (kAcross) {
+      if (!kFast) left = min(cols - column(i), kN);
+      if (last && k0 + row(i) >= K) left = 0;
+      return at[i] + (kMapped ? mapped(i, k0) : (int64_t)k0) * o.ld;
+    }
+    if (last) left = K - k0 - source(i) * kN;
+    return at[i] + k0;
+  }
+  // to `lds`; past the end zeros (kFast)
+  __device__ __forceinline__ void load(int i, int k0, char *lds) const {
+    int left;
+    const T *p = chunk(i, k0, left);
+    if (left <= 0) p = (const T *)&zero_chunk;
+    load_to_lds(p, lds + (i * kThreads + (threadIdx.x & ~63)) * 16);
+  }
+  // all chunks of the step are whole
+  __device__ __forceinline__ bool whole(int k0) const {
+    return k0 + kStep <= K && (!kAcross || col + kRows <= cols);
+  }
+  __device__ __forceinline__ Chunk fetch(int i, int k0, bool all) const {
+    int left;
+    const T *p = chunk(i, k0, left);
+    return __builtin_bit_cast(Chunk, all ? load_vec<T, false>(p, kN) : load_vec<T, true>(p, left));
   }
 };
 
-// Operand of rows r0..r0+15 of a tile, half `step` of its 128 bytes
-template <class T, bool kAcross, int kRows>
-__device__ __forceinline__ Frag<T> read_frag(const char *lds, int r0, int step) {
+// Operand of rows r0..r0+15 of a tile, `part` of its 64 bytes each
+template <class T, bool kAcross, int kRows, int kBytes>
+__device__ __forceinline__ Frag<T> read_frag(const char *lds, int r0, int part) {
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-  constexpr int kN = Vec<T>::kN, kChunks = kRows / kN;
+  constexpr int kN = Vec<T>::kN, kChunks = kAcross ? kRows / kN : kBytes / 16;
   Frag<T> f;
   if constexpr (!kAcross) {
     const int row = r0 + r;
-    f.v = *(const typename Vec<T>::V *)(lds + row * kStepBytes + ((step * 4 + g) ^ (row & 7)) * 16);
+    f.v = *(const typename Vec<T>::V *)(lds + row * kBytes +
+                                        chunk_place<T, false, kChunks>(row, part * 4 + g) * 16);
   } else if constexpr (sizeof(T) == 2) {
     // Two transposing reads: of the 16 lanes of a group lanes 4 j + i read 4
     // columns each of row j, and lane r gets column r of rows 0 to 3.
@@ -177,8 +196,9 @@ __device__ __forceinline__ Frag<T> read_frag(const char *lds, int r0, int step) 
     S4 h[2];
 #pragma unroll
     for (int j = 0; j < 2; j++) {
-      const int k = step * 32 + g * 8 + j * 4 + (r >> 2), c = r0 + (r & 3) * 4;
-      const char *p = lds + k * (kRows * 2) + across_place<T, kChunks>(k, c >> 3) * 16 + (c & 7) * 2;
+      const int k = part * 32 + g * 8 + j * 4 + (r >> 2), c = r0 + (r & 3) * 4;
+      const char *p = lds + k * (kRows * 2) + chunk_place<T, true, kChunks>(k, c >> 3) * 16 +
+                      (c & 7) * 2;
       h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) S4 *)p);
     }
     typedef short S8 __attribute__((ext_vector_type(8)));
@@ -188,9 +208,9 @@ __device__ __forceinline__ Frag<T> read_frag(const char *lds, int r0, int step) 
     const int c = r0 + r;
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-      const int k = step * 16 + g * 4 + i;
-      f.v[i] = *(const float *)(lds + k * (kRows * 4) + across_place<T, kChunks>(k, c >> 2) * 16 +
-                                (c & 3) * 4);
+      const int k = part * 16 + g * 4 + i;
+      f.v[i] = *(const float *)(lds + k * (kRows * 4) +
+                                chunk_place<T, true, kChunks>(k, c >> 2) * 16 + (c & 3) * 4);
     }
   }
   return f;
