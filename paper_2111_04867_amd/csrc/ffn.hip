@@ -188,20 +188,23 @@ __device__ __forceinline__ float sigmoid(float g) {
 }
 
 // A tile of BM rows by BN columns, by WM x WN wavefronts, over steps of kBytes
-// bytes of the shared axis, of which S lie in LDS.
-template <int M, int N, int kM, int kN, int B, int kS>
+// bytes of the shared axis, of which LDS holds SA of the rows and SB of the
+// columns.
+template <int M, int N, int kM, int kN, int B, int kA, int kB>
 struct Shape {
-  static constexpr int BM = M, BN = N, WM = kM, WN = kN, kBytes = B, S = kS;
-  static constexpr int kThreads = 64 * WM * WN, kLds = S * (BM + BN) * kBytes;
+  static constexpr int BM = M, BN = N, WM = kM, WN = kN, kBytes = B, SA = kA, SB = kB;
+  static constexpr int kThreads = 64 * WM * WN, kLds = (SA * BM + SB * BN) * kBytes;
 };
 
 template <class T, int kKind, bool kMapped, bool kFast, class Z>
 __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *lds) {
   constexpr bool kWeights = kKind == kDwOut || kKind == kDwIn;
   constexpr bool kAcrossA = kWeights, kAcrossB = kKind != kUp && kKind != kDown;
-  constexpr int BM = Z::BM, BN = Z::BN, WM = Z::WM, WN = Z::WN, kBytes = Z::kBytes, S = Z::S;
+  constexpr int BM = Z::BM, BN = Z::BN, WM = Z::WM, WN = Z::WN, kBytes = Z::kBytes;
+  constexpr int SA = Z::SA, SB = Z::SB;
   constexpr int kThreads = Z::kThreads, MI = BM / WM / 16, NI = BN / WN / 16;
-  constexpr int kBuffer = (BM + BN) * kBytes, kTileA = BM * kBytes;
+  constexpr int kTileA = BM * kBytes, kTileB = BN * kBytes;
+  char *const lds_b = lds + SA * kTileA;
   const int D = g.cols, F = g.hidden;
 
   // Blocks go to the XCDs in turn; 32 consecutive ones of an XCD take a piece
@@ -275,14 +278,14 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
   // A step's products, row of parts by row, whose operands are read two rows
   // ahead; `ahead(q)` is called before row q. The order is kept as it stands:
   // by itself the compiler reads an operand right where it is needed.
-  auto multiply_step = [&](const char *from, auto ahead) {
+  auto multiply_step = [&](const char *from_a, const char *from_b, auto ahead) {
     constexpr int kHalves = kBytes / 64, kDepth = MI < 2 ? 1 : 2;
     Frag<T> fa[kHalves][MI], fb[kHalves][NI];
     auto read_a = [&](int q) {
-      fa[q / MI][q % MI] = read_frag<T, kAcrossA, BM, kBytes>(from, wm + 16 * (q % MI), q / MI);
+      fa[q / MI][q % MI] = read_frag<T, kAcrossA, BM, kBytes>(from_a, wm + 16 * (q % MI), q / MI);
     };
     auto read_b = [&](int h, int j) {
-      fb[h][j] = read_frag<T, kAcrossB, BN, kBytes>(from + kTileA, wn + 16 * j, h);
+      fb[h][j] = read_frag<T, kAcrossB, BN, kBytes>(from_b, wn + 16 * j, h);
     };
 #pragma unroll
     for (int j = 0; j < NI; j++) read_b(0, j);
@@ -306,25 +309,34 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
   };
   if constexpr (kFast) {
     // Every step loads, past the end zeros that nothing uses, so that a step's
-    // loads are there when no more than those of S - 2 steps are on their way.
-    auto load = [&](int i, int s, char *to) {
-      if (i < la.kLoads) la.load(i, place(s), to);
-      else lb.load(i - la.kLoads, place(s), to + kTileA);
-    };
+    // loads are there when no more than those of SA - 2 and SB - 2 steps are on
+    // their way.
+    static_assert(SA >= SB && SB >= 2);
+    auto load_a = [&](int i, int s, char *to) { la.load(i, place(s), to); };
+    auto load_b = [&](int i, int s, char *to) { lb.load(i, place(s), to); };
 #pragma unroll
-    for (int s = 0; s < S - 1; s++)
+    for (int s = 0; s < SA - 1; s++) {
+      if (s < SB - 1)
 #pragma unroll
-      for (int i = 0; i < kLoads; i++) load(i, s, lds + s * kBuffer);
-    int now = 0;
+        for (int i = 0; i < lb.kLoads; i++) load_b(i, s, lds_b + s * kTileB);
+#pragma unroll
+      for (int i = 0; i < la.kLoads; i++) load_a(i, s, lds + s * kTileA);
+    }
+    int now_a = 0, now_b = 0;
     for (int s = 0; s < steps; s++) {
-      tile_barrier<kLoads *(S - 2)>();
-      char *next = lds + (now == 0 ? S - 1 : now - 1) * kBuffer;
-      multiply_step(lds + now * kBuffer, [&](int q) {
+      tile_barrier<la.kLoads *(SA - 2) + lb.kLoads *(SB - 2)>();
+      char *next_a = lds + (now_a == 0 ? SA - 1 : now_a - 1) * kTileA;
+      char *next_b = lds_b + (now_b == 0 ? SB - 1 : now_b - 1) * kTileB;
+      multiply_step(lds + now_a * kTileA, lds_b + now_b * kTileB, [&](int q) {
 #pragma unroll
-        for (int i = 0; i < kLoads; i++)
-          if (i >= q * kLoads / MI && i < (q + 1) * kLoads / MI) load(i, s + S - 1, next);
+        for (int i = 0; i < kLoads; i++) {
+          if (i < q * kLoads / MI || i >= (q + 1) * kLoads / MI) continue;
+          if (i < lb.kLoads) load_b(i, s + SB - 1, next_b);
+          else load_a(i - lb.kLoads, s + SA - 1, next_a);
+        }
       });
-      now = now == S - 1 ? 0 : now + 1;
+      now_a = now_a == SA - 1 ? 0 : now_a + 1;
+      now_b = now_b == SB - 1 ? 0 : now_b + 1;
     }
   } else {
     // chunks wait in registers, those of two steps on their way
@@ -341,18 +353,21 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
           h[i] = i < la.kLoads ? la.fetch(i, k0, false) : lb.fetch(i - la.kLoads, k0, false);
       }
     };
-    auto keep = [&](const Chunk(&h)[kLoads], char *to) {  // B's chunks lie behind A's
+    auto keep = [&](const Chunk(&h)[kLoads], int odd) {
 #pragma unroll
-      for (int i = 0; i < kLoads; i++) *(Chunk *)(to + (i * kThreads + threadIdx.x) * 16) = h[i];
+      for (int i = 0; i < kLoads; i++) {
+        char *to = i < la.kLoads ? lds + odd * kTileA : lds_b + odd * kTileB;
+        *(Chunk *)(to + ((i < la.kLoads ? i : i - la.kLoads) * kThreads + threadIdx.x) * 16) = h[i];
+      }
     };
     fetch(held[0], 0);
     fetch(held[1], 1);
-    keep(held[0], lds);
+    keep(held[0], 0);
     auto step = [&](int s, Chunk(&old)[kLoads], Chunk(&later)[kLoads]) {
       tile_barrier<63>();  // of LDS alone
       fetch(old, s + 2);
-      multiply_step(lds + (s & 1) * kBuffer, [](int) {});
-      keep(later, lds + (~s & 1) * kBuffer);
+      multiply_step(lds + (s & 1) * kTileA, lds_b + (s & 1) * kTileB, [](int) {});
+      keep(later, ~s & 1);
     };
     for (int s = 0; s < steps; s += 2) {
       step(s, held[0], held[1]);
@@ -430,12 +445,11 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
   }
 }
 
-using Tiny = Shape<32, 64, 2, 2, 128, 4>;
-using Small = Shape<64, 64, 2, 2, 128, 2>;
-using Medium = Shape<128, 128, 2, 2, 128, 2>;
-using Wide = Shape<128, 256, 2, 4, 128, 3>;
-using Large = Shape<256, 256, 2, 4, 128, 2>;
-using Deep = Shape<256, 256, 2, 4, 64, 5>;
+using Tiny = Shape<32, 64, 2, 2, 128, 4, 4>;
+using Small = Shape<64, 64, 2, 2, 128, 2, 2>;
+using Medium = Shape<128, 128, 2, 2, 128, 2, 2>;
+using Wide = Shape<128, 256, 2, 4, 128, 3, 3>;
+using Large = Shape<256, 256, 2, 4, 128, 3, 2>;
 enum Size { kTiny, kSmall, kMedium, kWide, kLarge };
 
 template <class T, int kKind, bool kMapped, bool kFast, class Z>
@@ -473,7 +487,7 @@ template <class T, int kKind, bool kMapped, bool kFast>
 Kernel kernel_of(Size size) {
 #define F(Z) shaped<Z>((const void *)ffn_product_kernel<T, kKind, kMapped, kFast, Z>)
   if constexpr (kKind == kDwOut || kKind == kDwIn) {  // smaller ones: ffn_last_kernel
-    if constexpr (kFast && sizeof(T) == 2) return size == kWide ? F(Wide) : F(Deep);
+    if constexpr (kFast && sizeof(T) == 2) return size == kWide ? F(Wide) : F(Large);
   } else {
     if constexpr (kFast && sizeof(T) == 2) {
       if (size == kWide) return F(Wide);
