@@ -25,8 +25,12 @@ struct FfnSpace {
   int64_t map;        // int32 [E][sources * capacity]: row numbers in the buffer (sources > 1)
   int64_t act;        // T [E][sources * capacity][hidden]
   int64_t dpre;       // T [E][sources * capacity][2 hidden] (backward)
+  int64_t done;       // int32 [4][kSplitTiles]: parts of a product's tiles that are there
+  int64_t partial;    // float: their sums
+  int64_t partial_bytes;
   int64_t bytes;
 };
+constexpr int kSplitTiles = 1024;
 FfnSpace ffn_space(int64_t sources, int64_t experts, int64_t capacity, int64_t hidden, int dtype,
                    bool backward);
 

@@ -51,7 +51,12 @@ FfnSpace ffn_space(int64_t sources, int64_t experts, int64_t capacity, int64_t h
   s.map = at;
   s.act = s.map + (sources > 1 ? rounded(4 * rows) : 0);
   s.dpre = s.act + rounded(rows * hidden * size);
-  s.bytes = s.dpre + (backward ? rounded(2 * rows * hidden * size) : 0);
+  s.done = s.dpre + (backward ? rounded(2 * rows * hidden * size) : 0);
+  s.partial = s.done + 4 * 4 * kSplitTiles;
+  // parts are worth it where a product has few tiles: small ones, and weights'
+  // gradients over many rows
+  s.partial_bytes = rounded(std::min<int64_t>(64 << 20, (3 << 18) + 64 * rows));
+  s.bytes = s.partial + s.partial_bytes;
   return s;
 }
 
@@ -65,6 +70,7 @@ struct PlanArgs {
   int32_t *rows, *num_tiles, *map;  // map: or null
   FfnTile *tiles[kLists];
   int32_t lists;  // bits: those that a product reads
+  int32_t *done;  // zeroed
   uint8_t *zero;  // rows past the counts are zeroed; or null
   int64_t row_bytes;
 };
@@ -97,6 +103,7 @@ __global__ __launch_bounds__(kPlanThreads) void ffn_plan_kernel(PlanArgs g) {
   __shared__ uint32_t from[kMaxExperts + 1];  // an expert's first tile, a source's first row
   const int E = g.experts, S = g.sources;
   if (blockIdx.x == 0) {
+    for (int i = threadIdx.x; i < 4 * kSplitTiles; i += kPlanThreads) g.done[i] = 0;
     for (int e = threadIdx.x; e < E; e += kPlanThreads) rows[e] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < S * E; i += kPlanThreads) atomicAdd(&rows[i % E], rows_of(g, i));
@@ -177,6 +184,9 @@ struct ProductArgs {
   int64_t slots;  // sources * capacity
   int32_t cols, hidden, experts;
   int32_t row_tiles, col_tiles;  // kDw*: tiles of an expert; else row_tiles is unused
+  int32_t parts;   // blocks that share a tile's steps
+  int32_t *done;   // [tiles]
+  float *partial;  // [tiles][parts][tile]
 };
 
 template <class T>
@@ -210,7 +220,8 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
   // Blocks go to the XCDs in turn; 32 consecutive ones of an XCD take a piece
   // of 8 tiles of columns by 4 of rows, whose operands its L2 holds.
   const uint32_t per_xcd = b >> 3;
-  const uint32_t id = ((per_xcd >> 5) * 8 + (b & 7)) * 32 + (per_xcd & 31);
+  const uint32_t place_of = ((per_xcd >> 5) * 8 + (b & 7)) * 32 + (per_xcd & 31);
+  const uint32_t id = place_of / (uint32_t)g.parts, part = place_of % (uint32_t)g.parts;
   const uint32_t entries = kWeights ? (uint32_t)(g.experts * g.row_tiles) : (uint32_t)*g.num_tiles;
   const uint32_t group = id / (entries * 8), width = min(8u, (uint32_t)g.col_tiles - group * 8);
   if (entries == 0 || group * 8 >= (uint32_t)g.col_tiles) return;
@@ -229,11 +240,14 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
   constexpr bool kBufferA = kKind == kUp || kKind == kGrad || kKind == kDwOut;
   const int lda = kKind == kDown ? F : kKind == kDx || kKind == kDwIn ? 2 * F : D;
   oa.p = (const T *)g.a + (kBufferA && map ? 0 : first * lda);
+  oa.end = (const T *)g.a + (int64_t)g.experts * g.slots * lda;
   oa.ld = lda;
   oa.map = kBufferA ? map : nullptr;
   const int ldb = kKind == kUp || kKind == kDx || kKind == kDwIn ? D : F;
   if (kWeights) ob.p = (const T *)g.b + (kKind == kDwIn && map ? 0 : first * ldb);
   else ob.p = (const T *)g.b + (int64_t)e * D * F * (kKind == kUp || kKind == kDx ? 2 : 1);
+  ob.end = (const T *)g.b + (kWeights ? g.slots * ldb
+                             : (int64_t)D * F * (kKind == kUp || kKind == kDx ? 2 : 1)) * g.experts;
   ob.ld = ldb;
   ob.map = kKind == kDwIn ? map : nullptr;
   const int K = kWeights ? n : kKind == kDown ? F : kKind == kDx ? 2 * F : D;
@@ -269,11 +283,15 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
     for (int j = 0; j < NI; j++) acc[i][j] = F4{0, 0, 0, 0};
 
   constexpr int kStep = kBytes / (int)sizeof(T);
-  const int steps = (K + kStep - 1) / kStep;
+  // this part's steps: from the `first_step`-th on
+  const int all_steps = (K + kStep - 1) / kStep;
+  const int first_step = (int)((int64_t)all_steps * part / g.parts);
+  const int steps = (int)((int64_t)all_steps * (part + 1) / g.parts) - first_step;
   constexpr int kLoads = la.kLoads + lb.kLoads;
-  const int turn = (int)((uint64_t)steps * (id >> 3 & 31) / 32);
-  auto place = [&](int s) {  // in the shared axis, of step s
-    return (s >= steps ? s : s + turn >= steps ? s + turn - steps : s + turn) * kStep;
+  const int turn = kFast ? (int)((uint64_t)steps * (id >> 3 & 31) / 32) : 0;
+  auto place = [&](int s) {  // in the shared axis, of step s; past the end its end
+    if (s >= steps) return all_steps * kStep;
+    return (first_step + (s + turn >= steps ? s + turn - steps : s + turn)) * kStep;
   };
   // A step's products, row of parts by row, whose operands are read two rows
   // ahead; `ahead(q)` is called before row q. The order is kept as it stands:
@@ -314,6 +332,14 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
     static_assert(SA >= SB && SB >= 2);
     auto load_a = [&](int i, int s, char *to) { la.load(i, place(s), to); };
     auto load_b = [&](int i, int s, char *to) { lb.load(i, place(s), to); };
+    // Rows looked up are waited for with all loads on their way, which are none
+    // behind the barrier of two steps.
+    static_assert(!kMapped || (SA == 2 && SB == 2));
+    auto look_up = [&](int s) {
+      la.look_up(place(s));
+      lb.look_up(place(s));
+    };
+    look_up(0);
 #pragma unroll
     for (int s = 0; s < SA - 1; s++) {
       if (s < SB - 1)
@@ -322,6 +348,7 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
 #pragma unroll
       for (int i = 0; i < la.kLoads; i++) load_a(i, s, lds + s * kTileA);
     }
+    look_up(1);
     int now_a = 0, now_b = 0;
     for (int s = 0; s < steps; s++) {
       tile_barrier<la.kLoads *(SA - 2) + lb.kLoads *(SB - 2)>();
@@ -334,24 +361,22 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
           if (i < lb.kLoads) load_b(i, s + SB - 1, next_b);
           else load_a(i - lb.kLoads, s + SA - 1, next_a);
         }
+        if (q == MI) look_up(s + 2);
       });
       now_a = now_a == SA - 1 ? 0 : now_a + 1;
       now_b = now_b == SB - 1 ? 0 : now_b + 1;
     }
   } else {
-    // chunks wait in registers, those of two steps on their way
+    // Chunks wait in registers, those of two steps on their way. Steps with parts
+    // of chunks come last, one at a time: their loads have branches, behind
+    // which the compiler waits for everything on its way (in one loop with the
+    // others the gradient of 32 x 640 rows of 2047 f16, hidden 1023, took 1399 us,
+    // 983 so).
     Chunk held[2][kLoads];
-    auto fetch = [&](Chunk(&h)[kLoads], int s) {
-      const int k0 = place(s);
-      if (la.whole(k0) && lb.whole(k0)) {
+    auto fetch = [&](Chunk(&h)[kLoads], int s, const auto &a, const auto &b) {
 #pragma unroll
-        for (int i = 0; i < kLoads; i++)
-          h[i] = i < la.kLoads ? la.fetch(i, k0, true) : lb.fetch(i - la.kLoads, k0, true);
-      } else {
-#pragma unroll
-        for (int i = 0; i < kLoads; i++)
-          h[i] = i < la.kLoads ? la.fetch(i, k0, false) : lb.fetch(i - la.kLoads, k0, false);
-      }
+      for (int i = 0; i < kLoads; i++)
+        h[i] = i < a.kLoads ? a.fetch_whole(i, place(s)) : b.fetch_whole(i - a.kLoads, place(s));
     };
     auto keep = [&](const Chunk(&h)[kLoads], int odd) {
 #pragma unroll
@@ -360,18 +385,43 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
         *(Chunk *)(to + ((i < la.kLoads ? i : i - la.kLoads) * kThreads + threadIdx.x) * 16) = h[i];
       }
     };
-    fetch(held[0], 0);
-    fetch(held[1], 1);
-    keep(held[0], 0);
-    auto step = [&](int s, Chunk(&old)[kLoads], Chunk(&later)[kLoads]) {
-      tile_barrier<63>();  // of LDS alone
-      fetch(old, s + 2);
-      multiply_step(lds + (s & 1) * kTileA, lds_b + (s & 1) * kTileB, [](int) {});
-      keep(later, ~s & 1);
+    const int whole = min(min(la.whole_steps(), lb.whole_steps()) - first_step, steps);
+    auto look_up = [&](int s) {
+      la.look_up(place(s));
+      lb.look_up(place(s));
     };
-    for (int s = 0; s < steps; s += 2) {
-      step(s, held[0], held[1]);
-      if (s + 1 < steps) step(s + 1, held[1], held[0]);
+    if (whole > 0) {
+      look_up(0);
+      fetch(held[0], 0, la, lb);
+      look_up(min(1, whole - 1));
+      fetch(held[1], min(1, whole - 1), la, lb);
+      look_up(min(2, whole - 1));
+      keep(held[0], 0);
+      auto step = [&](int s, Chunk(&old)[kLoads], Chunk(&later)[kLoads]) {
+        tile_barrier<63>();  // of LDS alone
+        const auto a = la;  // with the rows of this step
+        const auto b = lb;
+        look_up(min(s + 3, whole - 1));
+        fetch(old, min(s + 2, whole - 1), a, b);
+        multiply_step(lds + (s & 1) * kTileA, lds_b + (s & 1) * kTileB, [](int) {});
+        keep(later, ~s & 1);
+      };
+      int s = 0;
+      for (; s + 1 < whole; s += 2) {
+        step(s, held[0], held[1]);
+        step(s + 1, held[1], held[0]);
+      }
+      if (s < whole) step(s, held[0], held[1]);
+    }
+    for (int s = max(whole, 0); s < steps; s++) {
+      tile_barrier<63>();
+      look_up(s);
+#pragma unroll
+      for (int i = 0; i < kLoads; i++)
+        held[0][i] = i < la.kLoads ? la.fetch(i, place(s)) : lb.fetch(i - la.kLoads, place(s));
+      keep(held[0], 0);
+      tile_barrier<63>();
+      multiply_step(lds, lds_b, [](int) {});
     }
   }
 
@@ -380,6 +430,29 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
   // row's results leave in whole chunks next to each other (stored as they are,
   // 8 bytes here and there, the weights' gradient took three times as long).
   tile_barrier<0>();
+  if (g.parts > 1) {
+    const uint32_t tile = entry * g.col_tiles + tn;
+    float *sums = g.partial + (int64_t)tile * g.parts * (BM * BN) + threadIdx.x * 4;
+    auto at = [&](int p, int i, int j) {
+      return sums + ((int64_t)p * (MI * NI) + i * NI + j) * (kThreads * 4);
+    };
+#pragma unroll
+    for (int i = 0; i < MI; i++)
+#pragma unroll
+      for (int j = 0; j < NI; j++) put(at(part, i, j), acc[i][j]);
+    if (!last_of(g.done + tile, g.parts, (int32_t *)lds)) return;
+    // in their order, whichever was last
+#pragma unroll
+    for (int i = 0; i < MI; i++)
+#pragma unroll
+      for (int j = 0; j < NI; j++) acc[i][j] = get(at(0, i, j));
+    for (int p = 1; p < g.parts; p++)
+#pragma unroll
+      for (int i = 0; i < MI; i++)
+#pragma unroll
+        for (int j = 0; j < NI; j++) acc[i][j] += get(at(p, i, j));
+    __syncthreads();
+  }
   constexpr int kN = Vec<T>::kN, kPitch = 16 * NI * 4 + 16;
   constexpr int kPer = (kKind == kUp ? 8 : 16) * NI / kN;  // chunks of a row
   char *own = lds + wave * (16 * kPitch);
@@ -450,6 +523,8 @@ using Small = Shape<64, 64, 2, 2, 128, 2, 2>;
 using Medium = Shape<128, 128, 2, 2, 128, 2, 2>;
 using Wide = Shape<128, 256, 2, 4, 128, 3, 3>;
 using Large = Shape<256, 256, 2, 4, 128, 3, 2>;
+using MappedWide = Shape<128, 256, 2, 4, 128, 2, 2>;
+using MappedLarge = Shape<256, 256, 2, 4, 128, 2, 2>;
 enum Size { kTiny, kSmall, kMedium, kWide, kLarge };
 
 template <class T, int kKind, bool kMapped, bool kFast, class Z>
@@ -487,7 +562,10 @@ template <class T, int kKind, bool kMapped, bool kFast>
 Kernel kernel_of(Size size) {
 #define F(Z) shaped<Z>((const void *)ffn_product_kernel<T, kKind, kMapped, kFast, Z>)
   if constexpr (kKind == kDwOut || kKind == kDwIn) {  // smaller ones: ffn_last_kernel
-    if constexpr (kFast && sizeof(T) == 2) return size == kWide ? F(Wide) : F(Large);
+    if constexpr (kFast && sizeof(T) == 2) {
+      if constexpr (kMapped) return size == kWide ? F(MappedWide) : F(MappedLarge);
+      else return size == kWide ? F(Wide) : F(Large);
+    }
   } else {
     if constexpr (kFast && sizeof(T) == 2) {
       if (size == kWide) return F(Wide);
@@ -532,6 +610,9 @@ bool aligned16(P... p) {
 struct Products {
   ProductArgs base{};
   const FfnTile *tiles[kLists];
+  int32_t *done;
+  float *partial;
+  int64_t partial_bytes;
   bool fast;
   int dtype, cus;
   int64_t slots;
@@ -540,14 +621,42 @@ struct Products {
   int64_t count(int64_t m, int64_t n, int rows, int cols) const {
     return base.experts * ((m + rows - 1) / rows) * ((n + cols - 1) / cols);
   }
-  // Size of the tiles of a product of m rows and n columns per expert
+  // Size of the tiles of a product of m rows and n columns per expert: the one
+  // whose steps take the least time. A CU holds `held` blocks, which take `full`
+  // microseconds for a step of 128 bytes each, and `alone` if there is only one.
+  // Measured: f16 and bf16 with all CUs busy, on 64 x 980 x 4096 x 3 Ki (1434,
+  // 1571, 1773 and 2784 us from Large to Small), single blocks on 4 x 196 rows;
+  // in 32 bits the matrix instructions' time.
   Size size_of(int64_t m, int64_t n) const {
-    if (fast && dtype != TACCL_F32) {
-      if (count(m, n, 256, 256) >= 4 * cus) return kLarge;
-      if (4 * count(m, n, 128, 256) >= 3 * cus) return kWide;
-    }
-    if (2 * count(m, n, 128, 128) >= 3 * cus) return kMedium;
-    return count(m, n, 64, 64) >= cus ? kSmall : kTiny;
+    struct Cost {
+      Size size;
+      int rows, cols, held;
+      double full, alone;
+    };
+    static constexpr Cost k16[] = {{kLarge, 256, 256, 1, 1.75, 1.75},
+                                   {kWide, 128, 256, 1, 1.15, 1.1},
+                                   {kMedium, 128, 128, 2, 1.3, 0.8},
+                                   {kSmall, 64, 64, 4, 0.95, 0.5},
+                                   {kTiny, 32, 64, 2, 0.45, 0.45}};
+    static constexpr Cost k32[] = {{kMedium, 128, 128, 2, 3.4, 1.8},
+                                   {kSmall, 64, 64, 4, 1.8, 0.6},
+                                   {kTiny, 32, 64, 2, 0.6, 0.4}};
+    Size best = kMedium;
+    double least = 1e300;
+    auto consider = [&](const Cost &c) {
+      if (!fast && c.size >= kWide) return;
+      const double turns = (double)count(m, n, c.rows, c.cols) / (c.held * cus);
+      const double t = std::max(c.alone, turns * c.full);
+      if (t < least) {
+        least = t;
+        best = c.size;
+      }
+    };
+    if (dtype == TACCL_F32)
+      for (const Cost &c : k32) consider(c);
+    else
+      for (const Cost &c : k16) consider(c);
+    return best;
   }
 
   // the list that a product's kernel reads, as a bit
@@ -556,10 +665,10 @@ struct Products {
     const Kernel k = kernel_of<kKind>(dtype, base.map != nullptr, fast, size_of(m, n));
     return 1 << list_of(k.rows);
   }
-  // arguments of a product with this kernel's tiles, and its blocks
-  template <int kKind>
-  ProductArgs args(const Kernel &k, const void *a, const void *b, void *out, int64_t m, int64_t n,
-                   uint32_t &blocks) const {
+  // arguments of product `number` of a call with this kernel's tiles, over a
+  // shared axis of K, and its blocks; `used` bytes of the partial sums are taken
+  ProductArgs args(const Kernel &k, int number, const void *a, const void *b, void *out, int64_t m,
+                   int64_t n, int64_t K, uint32_t &blocks, int64_t &used) const {
     ProductArgs g = base;
     g.a = a;
     g.b = b;
@@ -568,17 +677,31 @@ struct Products {
     g.num_tiles += list_of(k.rows);
     g.col_tiles = (int)((n + k.cols - 1) / k.cols);
     g.row_tiles = (int)((m + k.rows - 1) / k.rows);
+    // Few tiles share their steps among parts, as many as CUs hold at two blocks
+    // each, of at least eight steps (2 x 340 rows of 4587 f32, hidden 32: 64 us a
+    // call without, 27 with).
+    const int64_t count = (int64_t)g.experts * g.row_tiles * g.col_tiles;
+    const int64_t step = dtype == TACCL_F32 ? 32 : 64, size = (int64_t)k.rows * k.cols * 4;
+    int64_t parts = 1;
+    if (count <= kSplitTiles)
+      parts = std::max<int64_t>(1, std::min({2 * (int64_t)cus / count, K / (8 * step), (int64_t)16,
+                                             (partial_bytes - used) / (count * size)}));
+    g.parts = (int)parts;
+    g.done = done + number * kSplitTiles;
+    g.partial = partial + used / 4;
+    if (parts > 1) used += count * parts * size;
     // ids come in pieces of 32 by 8 XCDs
-    blocks = out ? (uint32_t)(((int64_t)g.experts * g.row_tiles * g.col_tiles + 255) / 256 * 256) : 0;
+    blocks = out ? (uint32_t)((count * parts + 255) / 256 * 256) : 0;
     return g;
   }
-  // a product of m rows and n columns per expert
+  // a product of m rows and n columns per expert, alone in a launch
   template <int kKind>
-  hipError_t run(const void *a, const void *b, void *out, int64_t m, int64_t n,
-                 void *more = nullptr, const void *pre = nullptr) const {
+  hipError_t run(int number, const void *a, const void *b, void *out, int64_t m, int64_t n,
+                 int64_t K, void *more = nullptr, const void *pre = nullptr) const {
     const Kernel k = kernel_of<kKind>(dtype, base.map != nullptr, fast, size_of(m, n));
     uint32_t blocks;
-    ProductArgs g = args<kKind>(k, a, b, out, m, n, blocks);
+    int64_t used = 0;
+    ProductArgs g = args(k, number, a, b, out, m, n, K, blocks, used);
     g.more = more;
     g.pre = pre;
     void *p[] = {&g};
@@ -605,6 +728,9 @@ Products products(const A &a, const FfnSpace &sp, bool fast, int cus, hipStream_
   g.hidden = a.hidden;
   g.experts = a.num_experts;
   for (int i = 0; i < kLists; i++) p.tiles[i] = (const FfnTile *)(ws + sp.tiles[i]);
+  p.done = (int32_t *)(ws + sp.done);
+  p.partial = (float *)(ws + sp.partial);
+  p.partial_bytes = sp.partial_bytes;
   return p;
 }
 
@@ -621,6 +747,7 @@ hipError_t launch_plan(const A &a, const Products &p, int lists, void *zero) {
   q.map = (int32_t *)p.base.map;
   for (int i = 0; i < kLists; i++) q.tiles[i] = (FfnTile *)p.tiles[i];
   q.lists = lists;
+  q.done = p.done;
   q.zero = (uint8_t *)zero;
   q.row_bytes = a.cols * (a.dtype == TACCL_F32 ? 4 : 2);
   // four blocks per CU, in whole ones per piece
@@ -653,8 +780,8 @@ hipError_t launch_ffn(const taccl_ffn_t &a, int cus, hipStream_t stream) {
   void *act = (uint8_t *)a.workspace + sp.act;
   const int64_t D = a.cols, F = a.hidden;
   hipError_t e = launch_plan(a, p, p.list<kUp>(p.slots, 2 * F) | p.list<kDown>(p.slots, D), a.out);
-  if (e == hipSuccess) e = p.run<kUp>(a.buffer, a.w_in, act, p.slots, 2 * F, a.pre);
-  if (e == hipSuccess) e = p.run<kDown>(act, a.w_out, a.out, p.slots, D);
+  if (e == hipSuccess) e = p.run<kUp>(0, a.buffer, a.w_in, act, p.slots, 2 * F, D, a.pre);
+  if (e == hipSuccess) e = p.run<kDown>(1, act, a.w_out, a.out, p.slots, D, F);
   return e;
 }
 
@@ -670,9 +797,16 @@ hipError_t launch_ffn_backward(const taccl_ffn_backward_t &a, int cus, hipStream
   // Large products one by one, small ones together: alone they leave CUs empty.
   const bool each = fast && a.dtype != TACCL_F32 &&
                     std::min({p.size_of(p.slots, D), p.size_of(2 * F, D), p.size_of(D, F)}) >= kWide;
-  const int64_t tiles = p.count(p.slots, D, 128, 128) + p.count(2 * F, D, 128, 128) +
-                        p.count(D, F, 128, 128);
-  const Size size = tiles >= 8 * cus ? kMedium : kSmall;
+  // the longest tile alone, or all of them at full CUs
+  auto time = [&](int n, int held, double full, double alone) {
+    const double step = a.dtype == TACCL_F32 ? 32 : 64, by_f = 2 * F / step, by_rows = p.slots / step;
+    const double all = p.count(p.slots, D, n, n) * by_f +
+                       (p.count(2 * F, D, n, n) + p.count(D, F, n, n)) * by_rows;
+    return std::max(alone * std::max(by_f, by_rows), all * full / (held * cus));
+  };
+  const bool medium = a.dtype == TACCL_F32 ? time(128, 2, 3.4, 1.8) < time(64, 4, 1.8, 0.6)
+                                           : time(128, 2, 1.3, 0.8) < time(64, 4, 0.95, 0.5);
+  const Size size = medium ? kMedium : kSmall;
   const Kernel k = a.dtype == TACCL_F32    ? last_kernel<float>(mapped, fast, size)
                    : a.dtype == TACCL_BF16 ? last_kernel<bf16_t>(mapped, fast, size)
                                            : last_kernel<f16_t>(mapped, fast, size);
@@ -680,19 +814,20 @@ hipError_t launch_ffn_backward(const taccl_ffn_backward_t &a, int cus, hipStream
                              p.list<kGrad>(p.slots, F) |
                                  (each ? p.list<kDx>(p.slots, D) : 1 << list_of(k.rows)),
                              a.dbuffer);
-  if (e == hipSuccess) e = p.run<kGrad>(a.dout, a.w_out, dpre, p.slots, F, act, a.pre);
+  if (e == hipSuccess) e = p.run<kGrad>(0, a.dout, a.w_out, dpre, p.slots, F, D, act, a.pre);
   if (e != hipSuccess) return e;
   if (each) {
-    e = p.run<kDx>(dpre, a.w_in, a.dbuffer, p.slots, D);
-    if (e == hipSuccess) e = p.run<kDwIn>(dpre, a.buffer, a.dw_in, 2 * F, D);
-    if (e == hipSuccess) e = p.run<kDwOut>(a.dout, act, a.dw_out, D, F);
+    e = p.run<kDx>(1, dpre, a.w_in, a.dbuffer, p.slots, D, 2 * F);
+    if (e == hipSuccess) e = p.run<kDwIn>(2, dpre, a.buffer, a.dw_in, 2 * F, D, p.slots);
+    if (e == hipSuccess) e = p.run<kDwOut>(3, a.dout, act, a.dw_out, D, F, p.slots);
     return e;
   }
   LastArgs g{};
   uint32_t out_blocks;
-  g.dx = p.args<kDx>(k, dpre, a.w_in, a.dbuffer, p.slots, D, g.dx_blocks);
-  g.in = p.args<kDwIn>(k, dpre, a.buffer, a.dw_in, 2 * F, D, g.in_blocks);
-  g.out = p.args<kDwOut>(k, a.dout, act, a.dw_out, D, F, out_blocks);
+  int64_t used = 0;
+  g.out = p.args(k, 3, a.dout, act, a.dw_out, D, F, p.slots, out_blocks, used);
+  g.in = p.args(k, 2, dpre, a.buffer, a.dw_in, 2 * F, D, p.slots, g.in_blocks, used);
+  g.dx = p.args(k, 1, dpre, a.w_in, a.dbuffer, p.slots, D, 2 * F, g.dx_blocks, used);
   void *args[] = {&g};
   return hipLaunchKernel(k.fn, dim3(g.dx_blocks + g.in_blocks + out_blocks), dim3(k.threads), args,
                          k.lds, stream);

@@ -42,6 +42,33 @@ __device__ __forceinline__ void tile_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLater) : "memory");
 }
 
+// Stores and loads that other XCDs' blocks see and have made: a block that has
+// waited for its stores (vmcnt) and then counts itself as done, atomically, is
+// read by the one that finds all counted. Fences in their place write back and
+// drop a whole L2.
+__device__ __forceinline__ void put(float *p, F4 v) {
+#pragma unroll
+  for (int i = 0; i < 4; i++)
+    __hip_atomic_store(p + i, v[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ F4 get(const float *p) {
+  F4 v;
+#pragma unroll
+  for (int i = 0; i < 4; i++)
+    v[i] = __hip_atomic_load(p + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return v;
+}
+// By all threads of a block behind their put()s: whether it is the last of
+// `parts` blocks to come here. `word` lies in LDS.
+__device__ __forceinline__ bool last_of(int32_t *done, int parts, int32_t *word) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x == 0)
+    *word = __hip_atomic_fetch_add(done, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  __syncthreads();
+  return *word == parts - 1;
+}
+
 // One operand's part of a step: 16 rows by 64 bytes of the shared axis, a chunk
 // per lane. Lane l holds row l % 16; the elements of the shared axis are dealt
 // out to lane groups l / 16 alike for both operands.
@@ -63,10 +90,11 @@ __device__ __forceinline__ F4 multiply(const Frag<float> &a, const Frag<float> &
 }
 
 // An operand in memory: rows (tile rows where the shared axis is along them,
-// else rows of that axis) `ld` elements apart from `p`, or where `map` says.
+// else rows of that axis) `ld` elements apart from `p`, or where `map` says, of
+// an array that ends before `end`.
 template <class T>
 struct Operand {
-  const T *p;
+  const T *p, *end;
   int64_t ld;
   const int32_t *map;  // row numbers, or null
   __device__ __forceinline__ const T *row(int64_t i) const {
@@ -99,6 +127,7 @@ struct Loader {
   const T *at[kLoads];  // the chunk of the first step
   int K;                // the shared axis' length
   int col, cols;        // across: the tile's first column and their number
+  int32_t mapped[kMapped ? kLoads : 1];  // the rows of the next step to load
 
   static __device__ __forceinline__ int chunk_id(int i) { return i * kThreads + threadIdx.x; }
   // row of load i in LDS and the chunk of the operand that belongs there
@@ -131,22 +160,12 @@ struct Loader {
     const int c = col + source(i) * kN;
     return c < cols ? c : col;
   }
-  // The map's entry for row k of load i. A wavefront's load has few rows, whose
-  // entries are scalar loads: vector loads would be waited for behind all tiles
-  // on their way.
-  __device__ __forceinline__ int64_t mapped(int i, int k0) const {
-    constexpr int kPer = kChunks >= 64 ? 1 : 64 / kChunks;
-    typedef const __attribute__((address_space(4))) int32_t *Scalar;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int first = k0 + (i * kThreads + wave * 64) / kChunks;
-    const int mine = (threadIdx.x & 63) / kChunks;
-    int32_t at = 0;
+  // The map's entries for the step from k0 on, a step before its loads need them
+  // and ahead of those that are started between: loads arrive in order.
+  __device__ __forceinline__ void look_up(int k0) {
+    if (!kMapped) return;
 #pragma unroll
-    for (int j = 0; j < kPer; j++) {
-      const int32_t v = ((Scalar)(uintptr_t)o.map)[max(min(first + j, K - 1), 0)];
-      at = mine == j ? v : at;
-    }
-    return at;
+    for (int i = 0; i < kLoads; i++) mapped[i] = o.map[max(min(k0 + row(i), K - 1), 0)];
   }
 
   // Chunk i of the step from k0 on; `left` elements of it exist
@@ -156,7 +175,7 @@ struct Loader {
     if (kAcross) {
       if (!kFast) left = min(cols - column(i), kN);
       if (last && k0 + row(i) >= K) left = 0;
-      return at[i] + (kMapped ? mapped(i, k0) : (int64_t)k0) * o.ld;
+      return at[i] + (int64_t)(kMapped ? mapped[kMapped ? i : 0] : k0) * o.ld;
     }
     if (last) left = K - k0 - source(i) * kN;
     return at[i] + k0;
@@ -168,14 +187,30 @@ struct Loader {
     if (left <= 0) p = (const T *)&zero_chunk;
     load_to_lds(p, lds + (i * kThreads + (threadIdx.x & ~63)) * 16);
   }
-  // all chunks of the step are whole
-  __device__ __forceinline__ bool whole(int k0) const {
-    return k0 + kStep <= K && (!kAcross || col + kRows <= cols);
+  // Steps whose chunks can be read whole: to the shared axis' end along it; of
+  // an operand across it the last chunk of a row may reach into the next row
+  // (columns that are not stored), but not past the array.
+  __device__ __forceinline__ int whole_steps() const {
+    int n = K / kStep;
+    if (kAcross && col + kRows > cols) {
+      if (kMapped) {  // rows in ascending order: only the last may be the array's last
+        if (cols < kN) return 0;
+        if (n > 0 && n * kStep == K && o.end - o.row(K - 1) < cols + kN - 1) n--;
+        return n;
+      }
+      while (n > 0 && o.end - (o.p + ((int64_t)n * kStep - 1) * o.ld) < cols + kN - 1) n--;
+    }
+    return n;
   }
-  __device__ __forceinline__ Chunk fetch(int i, int k0, bool all) const {
+  // Chunk i of the step from k0 on, whole or as much of it as exists
+  __device__ __forceinline__ Chunk fetch_whole(int i, int k0) const {
+    int left;
+    return __builtin_bit_cast(Chunk, load_vec<T, false>(chunk(i, k0, left), kN));
+  }
+  __device__ __forceinline__ Chunk fetch(int i, int k0) const {
     int left;
     const T *p = chunk(i, k0, left);
-    return __builtin_bit_cast(Chunk, all ? load_vec<T, false>(p, kN) : load_vec<T, true>(p, left));
+    return __builtin_bit_cast(Chunk, load_vec<T, true>(p, left));
   }
 };
 

@@ -364,20 +364,6 @@ __global__ __launch_bounds__(kThreads, kPerCu) void tokens_up_kernel(TokensArgs 
   }
 }
 
-// Stores and loads that other XCDs' blocks see and have made
-__device__ __forceinline__ void put(float *p, F4 v) {
-#pragma unroll
-  for (int i = 0; i < 4; i++)
-    __hip_atomic_store(p + i, v[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ F4 get(const float *p) {
-  F4 v;
-#pragma unroll
-  for (int i = 0; i < 4; i++)
-    v[i] = __hip_atomic_load(p + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return v;
-}
-
 // 16 columns of the output, or a part of their sum: the entries' rows of w_out
 // one after the other are one long shared axis, dealt out to parts where the
 // columns alone make too few blocks. The last part to arrive adds them up, in
@@ -502,16 +488,7 @@ __global__ __launch_bounds__(kThreads, kDownPerCu<T>) void tokens_down_kernel(To
     const int64_t stride = (int64_t)(gridDim.x / g.parts) * a.tokens * 4;
     float *partial = (float *)(g.partial + ((int64_t)tile * a.tokens + t) * 4 + c);
     if (own) put(partial + part * stride * 4, y);
-    // the parts are there (atomic stores of the device's scope, waited for)
-    // before they are counted; fences, which write back and drop an L2, took
-    // ten times as long as the product
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (threadIdx.x == 0)
-      last = __hip_atomic_fetch_add(&g.chosen->done[tile], 1, __ATOMIC_RELAXED,
-                                    __HIP_MEMORY_SCOPE_AGENT) == g.parts - 1;
-    __syncthreads();
-    if (!last) return;
+    if (!last_of(&g.chosen->done[tile], g.parts, &last)) return;
     if (own) {
       y = get(partial);
       for (int p = 1; p < g.parts; p++) y += get(partial + p * stride * 4);
