@@ -223,26 +223,27 @@ def _gated(x, w_in, w_out, dtype, halves=1, weight=None):
     return y, 1.01 * slack, pre, pre_slack
 
 
-def ffn(buffer, counts, w_in, w_out):
-    """(out, its slack, pre, its slack), zero from the counts on."""
+def ffn(buffer, counts, w_in, w_out, device="cpu"):
+    """(out, its slack, pre, its slack), zero from the counts on; worked out on
+    `device`."""
     dtype, (s, e, c, d) = buffer.dtype, buffer.shape
     f = w_out.shape[2]
     n = held(counts, c)
-    out, slack = (torch.zeros(s, e, c, d, dtype=torch.float64) for _ in range(2))
-    pre, pre_slack = (torch.zeros(s, e, c, 2 * f, dtype=torch.float64) for _ in range(2))
-    x, wi, wo = (t.cpu().double() for t in (buffer, w_in, w_out))
+    out, slack, pre, pre_slack = (torch.zeros(s, e, c, k, dtype=torch.float64, device=device)
+                                  for k in (d, d, 2 * f, 2 * f))
+    x, wi, wo = (t.to(device).double() for t in (buffer, w_in, w_out))
     for j in range(e):
         for i in range(s):
             r = (i, j, slice(0, int(n[i, j])))
             out[r], slack[r], pre[r], pre_slack[r] = _gated(x[r], wi[j], wo[j], dtype)
-    return out, slack, pre, pre_slack
+    return tuple(t.cpu() for t in (out, slack, pre, pre_slack))
 
 
-def ffn_backward(dout, buffer, counts, w_in, w_out, pre):
+def ffn_backward(dout, buffer, counts, w_in, w_out, pre, device="cpu"):
     """((dbuffer, slack), (dw_in, slack), (dw_out, slack))."""
     dtype, (s, e, c, d) = buffer.dtype, buffer.shape
     n = held(counts, c)
-    dy, x, wi, wo, h = (t.cpu().double() for t in (dout, buffer, w_in, w_out, pre))
+    dy, x, wi, wo, h = (t.to(device).double() for t in (dout, buffer, w_in, w_out, pre))
     db, dbs = torch.zeros_like(x), torch.zeros_like(x)
     dwi, dwis, dwo, dwos = (torch.zeros_like(t) for t in (wi, wi, wo, wo))
     for j in range(e):
@@ -269,7 +270,7 @@ def ffn_backward(dout, buffer, counts, w_in, w_out, pre):
             dwis[j] += 1.01 * (dps.T @ x[r].abs() + rows * U * (dp.abs().T @ x[r].abs()))
             dwo[j] += dy[r].T @ a
             dwos[j] += 1.01 * (dy[r].abs().T @ a_s + rows * U * (dy[r].abs().T @ a.abs()))
-    return (db, dbs), (dwi, dwis), (dwo, dwos)
+    return tuple((a.cpu(), b.cpu()) for a, b in ((db, dbs), (dwi, dwis), (dwo, dwos)))
 
 
 def ffn_tokens(x, logits, k, w_in, w_out, mask=None, renorm=True, first=0):

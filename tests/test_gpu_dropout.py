@@ -45,6 +45,18 @@ def test_shares_and_ends():
     assert (out == 0).all()
 
 
+def test_rows_past_one_launch():
+    """2^21 rows of 8200 16-bit columns, 34 GB in place, take two launches."""
+    n, d = 1 << 21, 8200
+    x = torch.ones(n, d, dtype=torch.float16, device="cuda")
+    state = rng(9, 10)
+    X.dropout_tensors(x, state, x, p=0.5)
+    for first in (0, 1677720, n - 2):
+        later = rng(9, 10 + first * (d // 2)).cpu()
+        want = 2.0 * F.kept(later, 2, d, 0.5).half()
+        assert torch.equal(x[first:first + 2].cpu(), want)
+
+
 def test_what_is_dropped_is_not_looked_at():
     x = torch.full((64, 256), float("nan"), device="cuda")
     r = rows(3, 64, 256, torch.float32)
