@@ -42,7 +42,7 @@ struct Chosen {
   uint32_t tokens[kMaxEntries][2];  // bits
   int16_t experts[kMaxEntries];
   int16_t rows[kMaxEntries];  // the first token's row
-  int32_t done[kFfnMaxCols / 16];  // parts of a tile of columns that are there
+  int32_t done[kSplitTiles];  // parts of a tile of columns that are there
 };
 constexpr int64_t kChosenBytes = (sizeof(Chosen) + 255) / 256 * 256;
 
@@ -222,10 +222,10 @@ __device__ __forceinline__ void finish_step(Frag<T> *f, int step, int K) {
 }
 
 // w a of 8 hidden columns of an entry per turn: 8 gate and 8 up rows of its
-// expert's weights make one operand, its tokens the other; four wavefronts take
-// steps of 128 bytes in turn. The next steps are on their way while those
+// expert's weights make one operand, its tokens the other; kSplit wavefronts
+// take steps of 128 bytes in turn. The next steps are on their way while those
 // before are multiplied, across turns too.
-template <class T, bool kShort>
+template <class T, int kSplit, bool kShort>
 __global__ __launch_bounds__(kThreads, kPerCu) void tokens_up_kernel(TokensArgs g) {
   constexpr int U = 2;
   __shared__ Choices c;
@@ -251,19 +251,22 @@ __global__ __launch_bounds__(kThreads, kPerCu) void tokens_up_kernel(TokensArgs 
       g.chosen->experts[i] = (int16_t)e;
       g.chosen->rows[i] = c.rows[i];
     }
-    for (int i = threadIdx.x; i < (D + 15) / 16; i += kThreads) g.chosen->done[i] = 0;
+    for (int i = threadIdx.x; i < kSplitTiles; i += kThreads) g.chosen->done[i] = 0;
     if (threadIdx.x == 0) g.chosen->n = c.n;
   }
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
   const int steps = (D + kTokenStep<T> - 1) / kTokenStep<T>;
-  const int batches = (steps + U * kWaves - 1) / (U * kWaves);
+  const int batches = (steps + U * kSplit - 1) / (U * kSplit);
 
   struct Batch {
     Frag<T> w[U][2], x[U][2];
   };
+  constexpr int kGroups = kWaves / kSplit;  // of wavefronts, each with turns of its own
+  const int share = wave % kSplit, group = wave / kSplit;
+  const int start = blockIdx.x * kGroups + group, stride = gridDim.x * kGroups;
   // the next batch to load: its turn, place in it and operands
-  int next = blockIdx.x, part = 0;
+  int next = start, part = 0;
   const T *w = nullptr, *x = nullptr;
   auto load = [&](Batch &b) {
     if (next >= c.n * tiles) return;
@@ -276,7 +279,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void tokens_up_kernel(TokensArgs 
     }
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      const int s = (part * U + u) * kWaves + wave;
+      const int s = (part * U + u) * kSplit + share;
       if (s < steps) {
         load_step<T, kShort>(b.w[u], w, s, D);
         load_step<T, kShort>(b.x[u], x, s, D);
@@ -284,16 +287,16 @@ __global__ __launch_bounds__(kThreads, kPerCu) void tokens_up_kernel(TokensArgs 
     }
     if (++part == batches) {
       part = 0;
-      next += gridDim.x;
+      next += stride;
     }
   };
   F4 acc = {0, 0, 0, 0};
-  int item = blockIdx.x, done = 0;
+  int item = start, done = 0;
   uint32_t turns = 0;
   auto multiply_batch = [&](Batch &b) {
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      const int s = (done * U + u) * kWaves + wave;
+      const int s = (done * U + u) * kSplit + share;
       if (s < steps) {
         finish_step<T, kShort>(b.w[u], s, D);
         finish_step<T, kShort>(b.x[u], s, D);
@@ -304,23 +307,32 @@ __global__ __launch_bounds__(kThreads, kPerCu) void tokens_up_kernel(TokensArgs 
     if (++done < batches) return;
     done = 0;
     const uint32_t turn = turns & 1;
-    red[turn][wave][lane] = acc;
-    acc = F4{0, 0, 0, 0};
     const int f = item % tiles * 8 + 4 * q, slot = item / tiles;
-    item += gridDim.x;
-    lds_barrier();
+    item += stride;
+    F4 other = acc;  // the up rows' results
+    if (kSplit == 1) {
+#pragma unroll
+      for (int i = 0; i < 4; i++) other[i] = __shfl_xor(acc[i], 32);
+    } else {
+      red[turn][wave][lane] = acc;
+      lds_barrier();
+    }
     // the turns' sums go to the wavefronts in turn: lanes 0 to 31 take four
     // hidden columns of a token, whose gate rows they and whose up rows lanes 32
     // to 63 held
     const int e = c.list[slot] & (kMaxExperts - 1);
-    const int t = q < 2 && wave == (int)(turns & (kWaves - 1))
+    const int t = q < 2 && share == (int)(turns & (kSplit - 1))
                       ? token_of(c.tokens[e], (c.list[slot] >> 10) * 16 + r) : -1;
     if (t >= 0) {
-      F4 sg = red[turn][0][lane], su = red[turn][0][lane + 32];
+      F4 sg = acc, su = other;
+      if (kSplit > 1) {
+        sg = red[turn][0][lane];
+        su = red[turn][0][lane + 32];
 #pragma unroll
-      for (int v = 1; v < kWaves; v++) {
-        sg += red[turn][v][lane];
-        su += red[turn][v][lane + 32];
+        for (int v = 1; v < kSplit; v++) {
+          sg += red[turn][v][lane];
+          su += red[turn][v][lane + 32];
+        }
       }
       float weight = 0;
       for (int j = 0; j < a.k; j++)
@@ -350,6 +362,7 @@ __global__ __launch_bounds__(kThreads, kPerCu) void tokens_up_kernel(TokensArgs 
         *(T4 *)(row + g.wide) = lo;
       }
     }
+    acc = F4{0, 0, 0, 0};
     turns++;  // the other half's readers are behind this turn's barrier
   };
   Batch even, odd;
@@ -368,12 +381,21 @@ __global__ __launch_bounds__(kThreads, kPerCu) void tokens_up_kernel(TokensArgs 
 // one after the other are one long shared axis, dealt out to parts where the
 // columns alone make too few blocks. The last part to arrive adds them up, in
 // their order. Up to 16 tokens a column of the operand is a token; more are
-// added up per wavefront in LDS, entry by entry (kMany).
-template <class T, bool kMany, bool kShort>
+// added up per wavefront in LDS, entry by entry (kFold 0). Up to 8 (4) tokens
+// leave half (three quarters) of the operand's columns empty: they take the
+// tokens at the next step (three steps), and the other operand's rows are 8 (4)
+// columns of the output at both (four) steps. The results off this diagonal are
+// dropped, and there are two (four) times the tiles, which saves the parts: the
+// join takes about 3 us (4 tokens, 2 of 16 experts of 512 x 256 f32: 6.1 us with
+// four parts, 5.0 folded).
+template <class T, int kFold, bool kShort>
 __global__ __launch_bounds__(kThreads, kDownPerCu<T>) void tokens_down_kernel(TokensArgs g) {
   constexpr int U = 2, kPlanes = sizeof(T) == 4 ? 1 : 2;
-  constexpr int kCols = kMany ? kTokens : 16;
-  __shared__ F4 sums[kWaves][kCols][4];
+  constexpr bool kMany = kFold == 0;
+  constexpr int kSteps = kMany ? 1 : kFold;     // of an operand
+  constexpr int kRows = 16 / kSteps;            // columns of the output
+  constexpr int kTok = kMany ? kTokens : kRows;  // tokens
+  __shared__ F4 sums[kWaves * kSteps][kTok][kRows / 4];
   __shared__ uint32_t tokens[kMaxEntries][2];
   __shared__ int16_t experts[kMaxEntries], rows[kMaxEntries];
   __shared__ int last;
@@ -386,24 +408,33 @@ __global__ __launch_bounds__(kThreads, kDownPerCu<T>) void tokens_down_kernel(To
     rows[i] = g.chosen->rows[i];
     experts[i] = g.chosen->experts[i];
   }
-  for (int i = threadIdx.x; i < kWaves * kCols * 4; i += kThreads)
-    (&sums[0][0][0])[i] = F4{0, 0, 0, 0};
+  if (kMany)
+    for (int i = threadIdx.x; i < kWaves * kTok * (kRows / 4); i += kThreads)
+      (&sums[0][0][0])[i] = F4{0, 0, 0, 0};
   __syncthreads();
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
-  const int tile = blockIdx.x / g.parts, part = blockIdx.x % g.parts, d0 = tile * 16;
+  const int tile = blockIdx.x / g.parts, part = blockIdx.x % g.parts, d0 = tile * kRows;
   const int steps = (F + kTokenStep<T> - 1) / kTokenStep<T>;
 
   struct Batch {
     Frag<T> w[U][2], x[U][kPlanes][2];
     int slot[U], step[U];
   };
-  const T *first = (const T *)a.w_out + (int64_t)min(d0 + r, D - 1) * F;
-  // every kWaves-th of the part's steps
-  const int64_t all = (int64_t)n * steps, from = all * part / g.parts + wave;
-  const int64_t end = all * (part + 1) / g.parts;
-  const int count = from < end ? (int)((end - from + kWaves - 1) / kWaves) : 0;
-  int slot = count ? (int)(from / steps) : 0, s = count ? (int)(from % steps) : 0;
+  // rows and columns r, r + kRows, ... of the operands are at steps one later each
+  const int own = r % kRows, later = r / kRows;
+  const T *first = (const T *)a.w_out + (int64_t)min(d0 + own, D - 1) * F;
+  // of the part's steps every kWaves-th, or every kWaves-th few
+  const int64_t all = (int64_t)n * steps, begin = all * part / g.parts;
+  const int64_t end = all * (part + 1) / g.parts, from = begin + wave * kSteps;
+  const int count =
+      from < end ? (int)((end - from + kWaves * kSteps - 1) / (kWaves * kSteps)) : 0;
+  const int rest = (int)min(end - from - later, (int64_t)1 << 30);  // steps from the lane's first on
+  int slot = 0, s = 0;
+  if (count) {
+    slot = (int)((from + later) / steps);
+    s = (int)((from + later) % steps);
+  }
   int loaded = 0, done = 0;
   auto load = [&](Batch &b) {
 #pragma unroll
@@ -411,26 +442,32 @@ __global__ __launch_bounds__(kThreads, kDownPerCu<T>) void tokens_down_kernel(To
       if (loaded + u >= count) continue;
       b.slot[u] = slot;
       b.step[u] = s;
-      load_step<T, kShort>(b.w[u], first + (int64_t)experts[slot] * D * F, s, F);
+      const bool in = kSteps == 1 || (loaded + u) * (kWaves * kSteps) < rest;
+      if (kSteps > 1) {
+        b.w[u][0].v = b.w[u][1].v = typename Vec<T>::V{};
+      }
       // the token's row, or zeros
-      int row;
-      bool there;
-      const uint32_t low = tokens[slot][0], high = tokens[slot][1];
-      if (kMany) {
-        there = r < __popc(low) + __popc(high);
-        row = rows[slot] + r;
-      } else {
-        there = low >> r & 1;
-        row = rows[slot] + __popc(low & ((1u << r) - 1));
+      int row = 0;
+      bool there = false;
+      if (in) {
+        load_step<T, kShort>(b.w[u], first + (int64_t)experts[slot] * D * F, s, F);
+        const uint32_t low = tokens[slot][0], high = tokens[slot][1];
+        if (kMany) {
+          there = r < __popc(low) + __popc(high);
+          row = rows[slot] + r;
+        } else {
+          there = low >> own & 1;
+          row = rows[slot] + __popc(low & ((1u << own) - 1));
+        }
       }
 #pragma unroll
       for (int p = 0; p < kPlanes; p++) {
         b.x[u][p][0].v = b.x[u][p][1].v = typename Vec<T>::V{};
         if (there)
-          load_step<T, kShort>(b.x[u][p], (const T *)(g.act + (int64_t)row * g.wide * 4) + p * g.wide,
-                               s, F);
+          load_step<T, kShort>(b.x[u][p],
+                               (const T *)(g.act + (int64_t)row * g.wide * 4) + p * g.wide, s, F);
       }
-      s += kWaves;
+      s += kWaves * kSteps;
       while (s >= steps) {
         s -= steps;
         slot++;
@@ -471,30 +508,33 @@ __global__ __launch_bounds__(kThreads, kDownPerCu<T>) void tokens_down_kernel(To
     load(even);
     multiply_batch(odd);
   }
-  if (!kMany) sums[wave][r][q] = acc;
-  else if (count) flush();
+  if (kMany) {
+    if (count) flush();
+  } else if (q * 4 / kRows == later) {
+    sums[wave * kSteps + later][own][q % (kRows / 4)] = acc;
+  }
   __syncthreads();
 
   // thread (t, c): four columns of a token
-  const int t = threadIdx.x >> 2, c = threadIdx.x & 3;
-  const bool own = t < a.tokens;
+  const int t = threadIdx.x / (kRows / 4), c = threadIdx.x % (kRows / 4);
+  const bool mine = t < a.tokens;
   F4 y = {0, 0, 0, 0};
-  if (own) {
+  if (mine) {
     y = sums[0][t][c];
 #pragma unroll
-    for (int v = 1; v < kWaves; v++) y += sums[v][t][c];
+    for (int v = 1; v < kWaves * kSteps; v++) y += sums[v][t][c];
   }
   if (g.parts > 1) {
-    const int64_t stride = (int64_t)(gridDim.x / g.parts) * a.tokens * 4;
-    float *partial = (float *)(g.partial + ((int64_t)tile * a.tokens + t) * 4 + c);
-    if (own) put(partial + part * stride * 4, y);
+    const int64_t stride = (int64_t)(gridDim.x / g.parts) * a.tokens * (kRows / 4);
+    float *partial = (float *)(g.partial + ((int64_t)tile * a.tokens + t) * (kRows / 4) + c);
+    if (mine) put(partial + part * stride * 4, y);
     if (!last_of(&g.chosen->done[tile], g.parts, &last)) return;
-    if (own) {
+    if (mine) {
       y = get(partial);
       for (int p = 1; p < g.parts; p++) y += get(partial + p * stride * 4);
     }
   }
-  if (own) {
+  if (mine) {
     const int d = d0 + 4 * c;
     T *out = (T *)a.out + t * a.out_stride + d;
 #pragma unroll
@@ -503,18 +543,27 @@ __global__ __launch_bounds__(kThreads, kDownPerCu<T>) void tokens_down_kernel(To
   }
 }
 
-template <class T>
+template <class T, int kSplit>
 const void *up_fn(int cols) {
-  return cols < kTokenStep<T> ? (const void *)tokens_up_kernel<T, true>
-                              : (const void *)tokens_up_kernel<T, false>;
+  return cols < kTokenStep<T> ? (const void *)tokens_up_kernel<T, kSplit, true>
+                              : (const void *)tokens_up_kernel<T, kSplit, false>;
 }
 template <class T>
-const void *down_fn(int hidden, bool many) {
-  const bool brief = hidden < kTokenStep<T>;
-  return many ? (brief ? (const void *)tokens_down_kernel<T, true, true>
-                       : (const void *)tokens_down_kernel<T, true, false>)
-              : (brief ? (const void *)tokens_down_kernel<T, false, true>
-                       : (const void *)tokens_down_kernel<T, false, false>);
+const void *up_fn(int cols, bool split) {
+  return split ? up_fn<T, kWaves>(cols) : up_fn<T, 1>(cols);
+}
+
+template <class T, int kFold>
+const void *down_fn(int hidden) {
+  return hidden < kTokenStep<T> ? (const void *)tokens_down_kernel<T, kFold, true>
+                                : (const void *)tokens_down_kernel<T, kFold, false>;
+}
+template <class T>
+const void *down_fn(int hidden, int fold) {
+  return fold == 0   ? down_fn<T, 0>(hidden)
+         : fold == 1 ? down_fn<T, 1>(hidden)
+         : fold == 2 ? down_fn<T, 2>(hidden)
+                     : down_fn<T, 4>(hidden);
 }
 
 int64_t act_bytes(int64_t tokens, int64_t k, int64_t hidden) {
@@ -540,19 +589,30 @@ hipError_t launch_ffn_tokens(const taccl_ffn_tokens_t &a, int cus, hipStream_t s
   // entries, at most
   const int64_t choices = a.tokens * a.k;
   const int64_t most = std::min<int64_t>(choices, a.local_experts + choices / 16);
-  const int64_t blocks = std::min<int64_t>(most * (g.wide / 8), kPerCu * cus);
+  // Where every wavefront has turns of its own, a row of few steps stays with one,
+  // without a join per turn (us a call, shared and not: 20 tokens, 8 of 68 experts
+  // of 64 x 3392 f32 134 and 93; 16, 8 of 64 of 512 x 2048 bf16 92 and 81; 64, 8 of
+  // 64 of 1024 x 1024 120 and 116; but one token, 4 of 64 of 256 x 1024 10.9 and 11.6).
+  const int n = a.dtype == TACCL_F32 ? 4 : 8;
+  const int64_t turns = most * (g.wide / 8), row_steps = (a.cols + 8 * n - 1) / (8 * n);
+  const bool split = row_steps > 16 || turns < kWaves * kPerCu * cus;
+  const int64_t blocks =
+      std::min<int64_t>(split ? turns : (turns + kWaves - 1) / kWaves, kPerCu * cus);
   g.most = (int32_t)most;
-  hipError_t e = hipLaunchKernel(BY_TYPE(up_fn, a.cols), dim3((uint32_t)blocks), dim3(kThreads),
+  hipError_t e = hipLaunchKernel(BY_TYPE(up_fn, a.cols, split), dim3((uint32_t)blocks), dim3(kThreads),
                                  args, 0, stream);
   if (e != hipSuccess) return e;
-  // parts of at least four steps per wavefront, if that many entries are there
-  const int n = a.dtype == TACCL_F32 ? 4 : 8;
-  const int64_t tiles = (a.cols + 15) / 16, steps = most * ((a.hidden + 8 * n - 1) / (8 * n));
+  // the smallest tiles that the chip holds at once, then parts of at least eight
+  // operands' steps per wavefront, if that many entries are there
   const int64_t held = (a.dtype == TACCL_F32 ? kDownPerCu<float> : kDownPerCu<bf16_t>) * cus;
+  int fold = a.tokens > 16 ? 0 : a.tokens > 8 ? 1 : a.tokens > 4 ? 2 : 4;
+  auto tiles_of = [&](int64_t f) { return (a.cols * std::max<int64_t>(f, 1) + 15) / 16; };
+  while (fold > 1 && tiles_of(fold) > held) fold /= 2;
+  const int64_t tiles = tiles_of(fold), steps = most * ((a.hidden + 8 * n - 1) / (8 * n));
   g.parts = (int)std::max<int64_t>(
-      1, std::min<int64_t>({held / tiles, steps / (4 * kWaves), kMaxParts}));
-  return hipLaunchKernel(BY_TYPE(down_fn, a.hidden, a.tokens > 16),
-                         dim3((uint32_t)(tiles * g.parts)), dim3(kThreads), args, 0, stream);
+      1, std::min<int64_t>({held / tiles, steps / (8 * kWaves * std::max(fold, 1)), kMaxParts}));
+  return hipLaunchKernel(BY_TYPE(down_fn, a.hidden, fold), dim3((uint32_t)(tiles * g.parts)),
+                         dim3(kThreads), args, 0, stream);
 #undef BY_TYPE
 }
 

@@ -11,7 +11,10 @@ TYPES = pytest.mark.parametrize("dtype", F.TYPES.values(), ids=F.TYPES)
 # tokens, experts, k, dim, hidden
 CASES = [(1, 1, 1, 1, 1), (1, 8, 2, 64, 16), (2, 4, 4, 40, 24), (16, 16, 2, 72, 48),
          (17, 9, 3, 111, 77), (33, 70, 8, 130, 33), (64, 300, 16, 64, 32), (5, 1024, 4, 24, 8),
-         (3, 4, 2, 1111, 515), (32, 12, 5, 520, 264), (64, 3, 3, 2056, 72)]
+         (3, 4, 2, 1111, 515), (32, 12, 5, 520, 264), (64, 3, 3, 2056, 72),
+         # many turns of short rows; long sums for few columns, in parts
+         (20, 64, 4, 48, 700), (64, 40, 16, 130, 905), (3, 4, 2, 40, 6000), (8, 4, 2, 33, 4001),
+         (12, 6, 2, 50, 3008), (40, 5, 2, 9, 2500)]
 
 
 def make(dtype, t, e, k, d, f, seed=0, pad=0):
