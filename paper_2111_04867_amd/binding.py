@@ -52,7 +52,8 @@ EXPORTS = ["taccl_topology_create", "taccl_topology_destroy", "taccl_collective_
            "taccl_connections_batch", "taccl_generate_host", "taccl_count_faults",
            "taccl_norm", "taccl_norm_backward", "taccl_norm_workspace", "taccl_route",
            "taccl_route_backward", "taccl_route_workspace", "taccl_dispatch", "taccl_combine",
-           "taccl_combine_backward",
+           "taccl_combine_backward", "taccl_ffn", "taccl_ffn_backward", "taccl_ffn_workspace",
+           "taccl_ffn_tokens", "taccl_ffn_tokens_workspace", "taccl_dropout",
            "taccl_last_error",
            "taccl_version"]
 

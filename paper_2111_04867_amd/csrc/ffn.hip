@@ -9,6 +9,13 @@
 // numbers the rows below the counts, lists the tiles of rows that exist, and
 // zeroes the rows of the output past the counts. The products follow, two
 // forward and four backward, on the matrix units (tile.h).
+//
+// What bounds them: loads of tiles from L2, and what a tile does before its first
+// and behind its last step. 64 experts, 980 rows of 4096 bf16 each, hidden 1536: 1466
+// and 816 us forward (1070 and 960 TFLOP/s over the rows, 63 and 56% of the
+// matrix units' time; loading the tiles alone takes as long). The gradient of
+// 490 rows of 2048, hidden 1024: 246 us dg and du, 318 dx, 367 and 197 dw_in and
+// dw_out, which store 0.8 GB behind eight steps a tile.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -197,28 +204,29 @@ __device__ __forceinline__ float sigmoid(float g) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f));
 }
 
-// A tile of BM rows by BN columns, by WM x WN wavefronts, over steps of kBytes
-// bytes of the shared axis, of which LDS holds SA of the rows and SB of the
-// columns.
-template <int M, int N, int kM, int kN, int B, int kA, int kB>
+// A tile of BM rows by BN columns, by WM x WN wavefronts; LDS holds SA steps of
+// the rows and SB of the columns.
+template <int M, int N, int kM, int kN, int kA, int kB>
 struct Shape {
-  static constexpr int BM = M, BN = N, WM = kM, WN = kN, kBytes = B, SA = kA, SB = kB;
-  static constexpr int kThreads = 64 * WM * WN, kLds = (SA * BM + SB * BN) * kBytes;
+  static constexpr int BM = M, BN = N, WM = kM, WN = kN, SA = kA, SB = kB;
+  static constexpr int kThreads = 64 * WM * WN, kLds = (SA * BM + SB * BN) * kStepBytes;
 };
 
 template <class T, int kKind, bool kMapped, bool kFast, class Z>
 __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *lds) {
   constexpr bool kWeights = kKind == kDwOut || kKind == kDwIn;
   constexpr bool kAcrossA = kWeights, kAcrossB = kKind != kUp && kKind != kDown;
-  constexpr int BM = Z::BM, BN = Z::BN, WM = Z::WM, WN = Z::WN, kBytes = Z::kBytes;
+  constexpr int BM = Z::BM, BN = Z::BN, WM = Z::WM, WN = Z::WN;
   constexpr int SA = Z::SA, SB = Z::SB;
   constexpr int kThreads = Z::kThreads, MI = BM / WM / 16, NI = BN / WN / 16;
-  constexpr int kTileA = BM * kBytes, kTileB = BN * kBytes;
+  constexpr int kTileA = BM * kStepBytes, kTileB = BN * kStepBytes;
   char *const lds_b = lds + SA * kTileA;
   const int D = g.cols, F = g.hidden;
 
   // Blocks go to the XCDs in turn; 32 consecutive ones of an XCD take a piece
-  // of 8 tiles of columns by 4 of rows, whose operands its L2 holds.
+  // of 8 tiles of columns by 4 of rows, whose operands its L2 holds. The pieces'
+  // rows of tiles start at different steps: rows a power of two apart have one
+  // step in few of the L2's channels (1480 us to 1463 for the up projection).
   const uint32_t per_xcd = b >> 3;
   const uint32_t place_of = ((per_xcd >> 5) * 8 + (b & 7)) * 32 + (per_xcd & 31);
   const uint32_t id = place_of / (uint32_t)g.parts, part = place_of % (uint32_t)g.parts;
@@ -258,8 +266,8 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
   const int M = kKind == kDwOut ? D : kKind == kDwIn ? 2 * F : n;
   const int n0 = tn * kCols;
 
-  Loader<T, kAcrossA, kMapped && kKind == kDwOut, kFast, BM, kBytes, kThreads> la;
-  Loader<T, kAcrossB, kMapped && kKind == kDwIn, kFast, BN, kBytes, kThreads> lb;
+  Loader<T, kAcrossA, kMapped && kKind == kDwOut, kFast, BM, kThreads> la;
+  Loader<T, kAcrossB, kMapped && kKind == kDwIn, kFast, BN, kThreads> lb;
   if constexpr (kAcrossA) la.across(oa, K, t.row, M);
   else la.along(oa, K, [&](int r) { return min(t.row + r, M - 1); });
   if constexpr (kAcrossB) {
@@ -282,7 +290,7 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
 #pragma unroll
     for (int j = 0; j < NI; j++) acc[i][j] = F4{0, 0, 0, 0};
 
-  constexpr int kStep = kBytes / (int)sizeof(T);
+  constexpr int kStep = kStepBytes / (int)sizeof(T);
   // this part's steps: from the `first_step`-th on
   const int all_steps = (K + kStep - 1) / kStep;
   const int first_step = (int)((int64_t)all_steps * part / g.parts);
@@ -297,13 +305,13 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
   // ahead; `ahead(q)` is called before row q. The order is kept as it stands:
   // by itself the compiler reads an operand right where it is needed.
   auto multiply_step = [&](const char *from_a, const char *from_b, auto ahead) {
-    constexpr int kHalves = kBytes / 64, kDepth = MI < 2 ? 1 : 2;
+    constexpr int kHalves = 2, kDepth = MI < 2 ? 1 : 2;
     Frag<T> fa[kHalves][MI], fb[kHalves][NI];
     auto read_a = [&](int q) {
-      fa[q / MI][q % MI] = read_frag<T, kAcrossA, BM, kBytes>(from_a, wm + 16 * (q % MI), q / MI);
+      fa[q / MI][q % MI] = read_frag<T, kAcrossA, BM>(from_a, wm + 16 * (q % MI), q / MI);
     };
     auto read_b = [&](int h, int j) {
-      fb[h][j] = read_frag<T, kAcrossB, BN, kBytes>(from_b, wn + 16 * j, h);
+      fb[h][j] = read_frag<T, kAcrossB, BN>(from_b, wn + 16 * j, h);
     };
 #pragma unroll
     for (int j = 0; j < NI; j++) read_b(0, j);
@@ -428,7 +436,8 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
   // Lane l has columns l / 16 * 4 + 0..3 of row l % 16 of every 16 x 16 part.
   // Each wavefront passes 16 rows at a time through LDS of its own, so that a
   // row's results leave in whole chunks next to each other (stored as they are,
-  // 8 bytes here and there, the weights' gradient took three times as long).
+  // 8 bytes here and there, the four products of the gradient of 64 x 490 rows
+  // took 1583 us instead of 1440).
   tile_barrier<0>();
   if (g.parts > 1) {
     const uint32_t tile = entry * g.col_tiles + tn;
@@ -518,13 +527,15 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
   }
 }
 
-using Tiny = Shape<32, 64, 2, 2, 128, 4, 4>;
-using Small = Shape<64, 64, 2, 2, 128, 2, 2>;
-using Medium = Shape<128, 128, 2, 2, 128, 2, 2>;
-using Wide = Shape<128, 256, 2, 4, 128, 3, 3>;
-using Large = Shape<256, 256, 2, 4, 128, 3, 2>;
-using MappedWide = Shape<128, 256, 2, 4, 128, 2, 2>;
-using MappedLarge = Shape<256, 256, 2, 4, 128, 2, 2>;
+// LDS up to its 160 KB: as many bytes on their way as it holds (256 x 128: 2020 us
+// with two steps, 1701 with three for the up projection above)
+using Tiny = Shape<32, 64, 2, 2, 4, 4>;
+using Small = Shape<64, 64, 2, 2, 2, 2>;
+using Medium = Shape<128, 128, 2, 2, 2, 2>;
+using Wide = Shape<128, 256, 2, 4, 3, 3>;
+using Large = Shape<256, 256, 2, 4, 3, 2>;
+using MappedWide = Shape<128, 256, 2, 4, 2, 2>;
+using MappedLarge = Shape<256, 256, 2, 4, 2, 2>;
 enum Size { kTiny, kSmall, kMedium, kWide, kLarge };
 
 template <class T, int kKind, bool kMapped, bool kFast, class Z>

@@ -1,12 +1,13 @@
 // Matrix products on tiles in LDS for the experts' feed-forward (gfx950).
 //
 // A block multiplies BM rows of one operand by BN rows of the other over steps
-// of 64 or 128 bytes of the shared axis. Either operand is stored with the
+// of 128 bytes of the shared axis, a cache line of every row (steps of 64 bytes,
+// twice as many on their way, were 5 to 25% slower). Either operand is stored with the
 // shared axis contiguous ("along") or as rows of it ("across"); its tile lies
 // in LDS the way it is stored, in 16-byte chunks whose order within a row is
 // permuted so that the reads of a matrix instruction's operand touch every bank
-// equally often. Where every chunk is aligned and whole (kFast), loads go
-// straight to LDS, several steps ahead; else through registers, one ahead.
+// equally often (no conflict by the counters). Where every chunk is aligned and
+// whole (kFast), loads go straight to LDS; else through registers.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -17,6 +18,8 @@ namespace taccl {
 
 typedef float F4 __attribute__((ext_vector_type(4)));
 typedef uint32_t Chunk __attribute__((ext_vector_type(4)));
+
+constexpr int kStepBytes = 128;
 
 // what lanes past the shared axis' end load; never written
 static __device__ Chunk zero_chunk;
@@ -109,19 +112,19 @@ struct Operand {
 // each of 4 g + i.
 template <class T, bool kAcross, int kChunks>
 __device__ __forceinline__ int chunk_place(int r, int c) {
-  if (!kAcross) return c ^ (kChunks == 8 ? r & 7 : r >> 1 & 3);
+  if (!kAcross) return c ^ (r & 7);
   if (sizeof(T) == 2) return c ^ ((((r & 3) | (r >> 3 & 3) << 2) << 1) & (kChunks - 1));
   return c ^ (((r >> 2 & 3) << 2) & (kChunks - 1));
 }
 
 // The loads of an operand's tile of kRows rows (columns where the shared axis
-// is across) over kBytes bytes of the shared axis, by kThreads threads.
-template <class T, bool kAcross, bool kMapped, bool kFast, int kRows, int kBytes, int kThreads>
+// is across), by kThreads threads.
+template <class T, bool kAcross, bool kMapped, bool kFast, int kRows, int kThreads>
 struct Loader {
-  static constexpr int kLoads = kRows * kBytes / 16 / kThreads;
-  static constexpr int kN = Vec<T>::kN, kStep = kBytes / (int)sizeof(T);
-  static constexpr int kChunks = kAcross ? kRows / kN : kBytes / 16;  // per row in LDS
-  static_assert(kRows * kBytes / 16 % kThreads == 0);
+  static constexpr int kLoads = kRows * kStepBytes / 16 / kThreads;
+  static constexpr int kN = Vec<T>::kN, kStep = kStepBytes / (int)sizeof(T);
+  static constexpr int kChunks = kAcross ? kRows / kN : 8;  // per row in LDS
+  static_assert(kRows * 8 % kThreads == 0 && (kChunks & (kChunks - 1)) == 0);
 
   Operand<T> o;
   const T *at[kLoads];  // the chunk of the first step
@@ -214,15 +217,15 @@ struct Loader {
   }
 };
 
-// Operand of rows r0..r0+15 of a tile, `part` of its 64 bytes each
-template <class T, bool kAcross, int kRows, int kBytes>
+// Operand of rows r0..r0+15 of a tile, half `part` of its step
+template <class T, bool kAcross, int kRows>
 __device__ __forceinline__ Frag<T> read_frag(const char *lds, int r0, int part) {
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-  constexpr int kN = Vec<T>::kN, kChunks = kAcross ? kRows / kN : kBytes / 16;
+  constexpr int kN = Vec<T>::kN, kChunks = kAcross ? kRows / kN : 8;
   Frag<T> f;
   if constexpr (!kAcross) {
     const int row = r0 + r;
-    f.v = *(const typename Vec<T>::V *)(lds + row * kBytes +
+    f.v = *(const typename Vec<T>::V *)(lds + row * kStepBytes +
                                         chunk_place<T, false, kChunks>(row, part * 4 + g) * 16);
   } else if constexpr (sizeof(T) == 2) {
     // Two transposing reads: of the 16 lanes of a group lanes 4 j + i read 4
