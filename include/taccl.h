@@ -629,10 +629,12 @@ taccl_status_t taccl_ffn_backward(const taccl_ffn_backward_t *a, taccl_stream_t 
  * whose weights w_in and w_out hold: a rank with some of the experts gives its
  * part, and the ranks' parts add up to the layer. Zero for a token without such
  * a choice. weights[t][j] * a is held in 32 bits (TACCL_F32) or as the sum of
- * two numbers of the type (16 bits; past 65504 in TACCL_F16 it is infinite).
+ * two numbers of the type (16 bits; past 65504 in TACCL_F16 it is infinite, and
+ * its product with an infinite weight of Wo may be NaN).
  * experts and weights [tokens][k]: or NULL.
  * 0 <= tokens <= 64, E <= 1024, k <= min(E, 16), cols, hidden <= 65536.
- * `workspace`: taccl_ffn_tokens_workspace(tokens, k, cols, hidden) bytes, 16-byte aligned, not shared with another call in flight.
+ * `workspace`: taccl_ffn_tokens_workspace(tokens, k, cols, hidden) bytes,
+ * 16-byte aligned, not shared with another call in flight.
  */
 typedef struct {
   int64_t tokens;

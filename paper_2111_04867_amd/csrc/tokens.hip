@@ -420,6 +420,7 @@ __global__ __launch_bounds__(kThreads, kDownPerCu<T>) void tokens_down_kernel(To
   struct Batch {
     Frag<T> w[U][2], x[U][kPlanes][2];
     int slot[U], step[U];
+    bool there[U];
   };
   // rows and columns r, r + kRows, ... of the operands are at steps one later each
   const int own = r % kRows, later = r / kRows;
@@ -448,7 +449,8 @@ __global__ __launch_bounds__(kThreads, kDownPerCu<T>) void tokens_down_kernel(To
       }
       // the token's row, or zeros
       int row = 0;
-      bool there = false;
+      bool &there = b.there[u];
+      there = false;
       if (in) {
         load_step<T, kShort>(b.w[u], first + (int64_t)experts[slot] * D * F, s, F);
         const uint32_t low = tokens[slot][0], high = tokens[slot][1];
@@ -491,12 +493,16 @@ __global__ __launch_bounds__(kThreads, kDownPerCu<T>) void tokens_down_kernel(To
         now = b.slot[u];
       }
       finish_step<T, kShort>(b.w[u], b.step[u], F);
+      F4 sum = acc;
 #pragma unroll
       for (int p = 0; p < kPlanes; p++) {
         finish_step<T, kShort>(b.x[u][p], b.step[u], F);
 #pragma unroll
-        for (int h = 0; h < 2; h++) acc = multiply(b.w[u][h], b.x[u][p][h], acc);
+        for (int h = 0; h < 2; h++) sum = multiply(b.w[u][h], b.x[u][p][h], sum);
       }
+      // zero times an infinite or NaN weight of an expert that the token did not choose
+#pragma unroll
+      for (int i = 0; i < 4; i++) acc[i] = kMany || b.there[u] ? sum[i] : acc[i];
     }
     done += U;
   };

@@ -110,6 +110,28 @@ def test_the_routers_choices():
         assert out[fine].isfinite().all() and int(fine.sum()) >= 38
 
 
+@TYPES
+@pytest.mark.parametrize("case", [(3, 6, 2, 40, 264), (4, 6, 2, 40, 24), (8, 6, 2, 40, 264),
+                                  (7, 6, 2, 600, 24), (16, 6, 2, 40, 264), (13, 6, 1, 40, 4000),
+                                  (40, 6, 2, 40, 264), (64, 6, 1, 40, 24)], ids=str)
+@pytest.mark.parametrize("value", [float("nan"), float("inf")], ids=str)
+def test_weights_of_experts_not_chosen(dtype, case, value):
+    """An expert that has diverged changes its own tokens alone."""
+    m = make(dtype, *case, seed=5)
+    m["logits"][0, 1] = 50
+    m["logits"][1, 1] = -50
+    clean, experts, _ = run(m, case[2])
+    for name in ("w_in", "w_out"):
+        kept = m[name][1].clone()
+        m[name][1] = value
+        out = run(m, case[2])[0]
+        m[name][1] = kept
+        own = (experts == 1).any(1)
+        assert 0 < int(own.sum()) < case[0]
+        assert torch.equal(out[~own], clean[~own])
+        assert not out[own].isfinite().any()
+
+
 @pytest.mark.parametrize("logits", F.TYPES.values(), ids=F.TYPES)
 def test_types_of_logits(logits):
     m = make(torch.bfloat16, 9, 30, 4, 64, 32, seed=4)
