@@ -16,6 +16,12 @@ for any kernel. `norm`, `route`, `dispatch`, `ffn`, `combine` and `dropout`
 allocate their results and are differentiable, once: a second derivative
 raises. `ffn_tokens` allocates its results and has no gradient. There is no
 fallback: without the library they raise.
+
+All calls can be captured into a graph. For a gradient torch asks that no
+autograd graph of an earlier pass over the same leaves is alive when a pass is
+captured (it adds to a leaf's gradient on the stream of the first one, which is
+not the captured one): drop the earlier results first, or capture over leaves of
+its own.
 """
 import ctypes as ct
 

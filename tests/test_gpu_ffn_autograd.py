@@ -205,6 +205,43 @@ def test_in_graphs(sizes):
                 assert torch.equal(a, b)
 
 
+def test_a_captured_gradient():
+    """Forward and gradient in one graph: replays draw new random numbers and
+    give the eager results' bits. Every pass has leaves of its own."""
+    values = layer(torch.bfloat16, e=3, c=40, d=72, f=40)
+    counts, rng = values[1], torch.tensor([5, 0], device="cuda")
+    dout = randn(7, 3 * 40, 72).bfloat16()
+
+    def step(leaves):
+        out = X.ffn(leaves[0], counts, *leaves[1:]).view(3 * 40, 72)
+        out = X.dropout(out, 0.3, rng, leaves[0].view(3 * 40, 72))
+        return [out.detach(), *torch.autograd.grad(out, leaves, dout)]
+
+    def leaves():
+        return [values[i].clone().requires_grad_() for i in (0, 2, 3)]
+
+    own = leaves()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(leaves())
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step(own)
+    last = None
+    for i in range(4):
+        rng[1] += X.dropout_words(120, 72)
+        want = step(leaves())
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(held, want):
+            assert torch.equal(a, b)
+        assert last is None or not torch.equal(last, held[0])
+        last = held[0].clone()
+
+
 @pytest.mark.parametrize("dtype", F.TYPES.values(), ids=F.TYPES)
 def test_the_layer_in_parts_and_whole(dtype):
     """norm, route, dispatch, ffn, combine and dropout as a layer runs them; the

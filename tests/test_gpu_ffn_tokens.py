@@ -132,6 +132,32 @@ def test_weights_of_experts_not_chosen(dtype, case, value):
         assert not out[own].isfinite().any()
 
 
+@TYPES
+@pytest.mark.parametrize("t", [1, 16, 64])
+def test_no_choices(dtype, t):
+    """Nothing is read of weights that no token chose."""
+    m = make(dtype, t, 6, 2, 40, 264, seed=6)
+    m["w_in"][:], m["w_out"][:] = float("nan"), float("nan")
+    for options in ({"mask": torch.zeros(t, dtype=torch.bool, device="cuda")}, {}):
+        if not options:
+            m["logits"][:] = float("-inf")
+        out, experts, weights = run(m, 2, **options)
+        assert (out == 0).all() and (experts == -1).all() and (weights == 0).all()
+
+
+@TYPES
+@pytest.mark.parametrize("t", [3, 8, 16, 40])
+def test_tokens_are_apart(dtype, t):
+    """A token that is not finite leaves the others as they were."""
+    m = make(dtype, t, 4, 3, 72, 136, seed=7)
+    clean = run(m, 3)[0]
+    m["x"][1] = float("nan")
+    m["x"][2, 5] = float("inf")
+    out = run(m, 3)[0]
+    assert torch.equal(out[0], clean[0]) and torch.equal(out[3:], clean[3:])
+    assert not out[1:3].isfinite().any()
+
+
 @pytest.mark.parametrize("logits", F.TYPES.values(), ids=F.TYPES)
 def test_types_of_logits(logits):
     m = make(torch.bfloat16, 9, 30, 4, 64, 32, seed=4)
