@@ -60,9 +60,9 @@ FfnSpace ffn_space(int64_t sources, int64_t experts, int64_t capacity, int64_t h
   s.dpre = s.act + rounded(rows * hidden * size);
   s.done = s.dpre + (backward ? rounded(2 * rows * hidden * size) : 0);
   s.partial = s.done + 4 * 4 * kSplitTiles;
-  // parts are worth it where a product has few tiles: small ones, and weights'
-  // gradients over many rows
-  s.partial_bytes = rounded(std::min<int64_t>(64 << 20, (3 << 18) + 64 * rows));
+  // parts are worth it where a product has few tiles, small ones, and weights'
+  // gradients over many rows, or few in its last turn
+  s.partial_bytes = rounded(std::min<int64_t>(64 << 20, (3 << 18) + 4096 * rows));
   s.bytes = s.partial + s.partial_bytes;
   return s;
 }
@@ -192,6 +192,9 @@ struct ProductArgs {
   int32_t cols, hidden, experts;
   int32_t row_tiles, col_tiles;  // kDw*: tiles of an expert; else row_tiles is unused
   int32_t parts;   // blocks that share a tile's steps
+  // The chip holds `round` blocks (0: not looked at). Where the last tiles are
+  // fewer, up to `last_parts` blocks share one of them, `room` parts in all.
+  uint32_t round, last_parts, room;
   int32_t *done;   // [tiles]
   float *partial;  // [tiles][parts][tile]
 };
@@ -229,8 +232,16 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
   // step in few of the L2's channels (1480 us to 1463 for the up projection).
   const uint32_t per_xcd = b >> 3;
   const uint32_t place_of = ((per_xcd >> 5) * 8 + (b & 7)) * 32 + (per_xcd & 31);
-  const uint32_t id = place_of / (uint32_t)g.parts, part = place_of % (uint32_t)g.parts;
   const uint32_t entries = kWeights ? (uint32_t)(g.experts * g.row_tiles) : (uint32_t)*g.num_tiles;
+  uint32_t parts = (uint32_t)g.parts, alone = 0;  // tiles that are not shared
+  if (g.round) {
+    const uint32_t all = entries * (uint32_t)g.col_tiles, last = all % g.round;
+    if (last && place_of >= all - last) {
+      parts = max(1u, min(g.last_parts, g.room / last));
+      alone = all - last;
+    }
+  }
+  const uint32_t id = alone + (place_of - alone) / parts, part = (place_of - alone) % parts;
   const uint32_t group = id / (entries * 8), width = min(8u, (uint32_t)g.col_tiles - group * 8);
   if (entries == 0 || group * 8 >= (uint32_t)g.col_tiles) return;
   const uint32_t in = id - group * entries * 8, entry = in / width;
@@ -293,8 +304,8 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
   constexpr int kStep = kStepBytes / (int)sizeof(T);
   // this part's steps: from the `first_step`-th on
   const int all_steps = (K + kStep - 1) / kStep;
-  const int first_step = (int)((int64_t)all_steps * part / g.parts);
-  const int steps = (int)((int64_t)all_steps * (part + 1) / g.parts) - first_step;
+  const int first_step = (int)((int64_t)all_steps * part / parts);
+  const int steps = (int)((int64_t)all_steps * (part + 1) / parts) - first_step;
   constexpr int kLoads = la.kLoads + lb.kLoads;
   const int turn = kFast ? (int)((uint64_t)steps * (id >> 3 & 31) / 32) : 0;
   auto place = [&](int s) {  // in the shared axis, of step s; past the end its end
@@ -439,27 +450,25 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
   // 8 bytes here and there, the four products of the gradient of 64 x 490 rows
   // took 1583 us instead of 1440).
   tile_barrier<0>();
-  if (g.parts > 1) {
-    const uint32_t tile = entry * g.col_tiles + tn;
-    float *sums = g.partial + (int64_t)tile * g.parts * (BM * BN) + threadIdx.x * 4;
-    auto at = [&](int p, int i, int j) {
-      return sums + ((int64_t)p * (MI * NI) + i * NI + j) * (kThreads * 4);
-    };
+  if (parts > 1) {
+    const uint32_t tile = id - alone;
+    constexpr int kAll = MI * NI, kOnce = kAll < 16 ? kAll : 16;
+    float *sums = g.partial + (int64_t)tile * parts * (BM * BN) + wave * (kAll * 256) + lane * 4;
 #pragma unroll
-    for (int i = 0; i < MI; i++)
-#pragma unroll
-      for (int j = 0; j < NI; j++) put(at(part, i, j), acc[i][j]);
-    if (!last_of(g.done + tile, g.parts, (int32_t *)lds)) return;
+    for (int i = 0; i < kAll; i++) put_chunk(sums + part * (BM * BN) + i * 256, acc[i / NI][i % NI]);
+    if (!last_of(g.done + tile, (int)parts, (int32_t *)lds)) return;
     // in their order, whichever was last
+    for (int p = 0; p < (int)parts; p++)
 #pragma unroll
-    for (int i = 0; i < MI; i++)
+      for (int i0 = 0; i0 < kAll; i0 += kOnce) {
+        F4 v[kOnce];
+        get_chunks(v, sums + p * (BM * BN) + i0 * 256);
 #pragma unroll
-      for (int j = 0; j < NI; j++) acc[i][j] = get(at(0, i, j));
-    for (int p = 1; p < g.parts; p++)
-#pragma unroll
-      for (int i = 0; i < MI; i++)
-#pragma unroll
-        for (int j = 0; j < NI; j++) acc[i][j] += get(at(p, i, j));
+        for (int i = 0; i < kOnce; i++) {
+          F4 &sum = acc[(i0 + i) / NI][(i0 + i) % NI];
+          sum = p ? sum + v[i] : v[i];
+        }
+      }
     __syncthreads();
   }
   constexpr int kN = Vec<T>::kN, kPitch = 16 * NI * 4 + 16;
@@ -564,6 +573,7 @@ __global__ __launch_bounds__(Z::kThreads, Z::BM == 64 ? 4 : 2) void ffn_last_ker
 struct Kernel {
   const void *fn;
   int rows, cols, threads, lds;
+  int held() const { return cols == 256 ? 1 : rows == 64 ? 4 : 2; }  // blocks of a CU
 };
 template <class Z>
 Kernel shaped(const void *fn) {
@@ -689,13 +699,13 @@ struct Products {
     g.col_tiles = (int)((n + k.cols - 1) / k.cols);
     g.row_tiles = (int)((m + k.rows - 1) / k.rows);
     // Few tiles share their steps among parts, as many as CUs hold at two blocks
-    // each, of at least eight steps (2 x 340 rows of 4587 f32, hidden 32: 64 us a
+    // each (one of the largest tiles), of at least eight steps (2 x 340 rows of 4587 f32, hidden 32: 64 us a
     // call without, 27 with).
     const int64_t count = (int64_t)g.experts * g.row_tiles * g.col_tiles;
     const int64_t step = dtype == TACCL_F32 ? 32 : 64, size = (int64_t)k.rows * k.cols * 4;
     int64_t parts = 1;
     if (count <= kSplitTiles)
-      parts = std::max<int64_t>(1, std::min({2 * (int64_t)cus / count, K / (8 * step), (int64_t)16,
+      parts = std::max<int64_t>(1, std::min({std::min(2, k.held()) * (int64_t)cus / count, K / (8 * step), (int64_t)16,
                                              (partial_bytes - used) / (count * size)}));
     g.parts = (int)parts;
     g.done = done + number * kSplitTiles;
@@ -713,6 +723,21 @@ struct Products {
     uint32_t blocks;
     int64_t used = 0;
     ProductArgs g = args(k, number, a, b, out, m, n, K, blocks, used);
+    // The tiles of rows that exist may leave most of the chip without one in its
+    // last turn, which only the device knows: up to four blocks share such a tile,
+    // of at least eight steps each (us a call without and so: 8 x 600 rows of 2048
+    // f32, hidden 1024 654 and 554; 4 x 1030 bf16 105 and 102; gradient of 6 x 700
+    // bf16, hidden 1408 281 and 260, of 8 x 200 of 4096, hidden 1536 303 and 286).
+    // Through registers sixteen (20 x 500 rows of 2047 f16, hidden 1023: 247 us
+    // without, 263 with eight).
+    const int64_t steps = K / (dtype == TACCL_F32 ? 32 : 64), round = (int64_t)cus * k.held();
+    const int64_t last_parts = std::min<int64_t>(steps / (fast ? 8 : 16), 4);
+    if (g.parts == 1 && last_parts > 1 && round <= kSplitTiles && round % 256 == 0) {
+      g.round = (uint32_t)round;
+      g.last_parts = (uint32_t)last_parts;
+      g.room = (uint32_t)std::min(round, partial_bytes / ((int64_t)k.rows * k.cols * 4));
+      blocks = (uint32_t)((blocks + round - 1) / round * round);
+    }
     g.more = more;
     g.pre = pre;
     void *p[] = {&g};

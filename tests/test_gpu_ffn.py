@@ -24,6 +24,9 @@ LONG = [(1, 2, 40, 4104, 32), (3, 2, 13, 4101, 33), (1, 1, 3000, 64, 32), (8, 1,
 LARGE = [(1, 130, 260, 264, 136), (2, 128, 140, 512, 264), (4, 16, 300, 1032, 520),
          (2, 16, 256, 1024, 512), (1, 24, 300, 777, 333), (1, 20, 512, 1024, 512),
          (2, 8, 300, 1024, 510)]
+# a last turn of few tiles, which blocks share; so, in 32 bits, and by registers
+LAST = [(1, 4, 1100, 1032, 1024), (2, 8, 310, 2048, 512), (1, 6, 700, 2049, 255),
+        (3, 7, 150, 1025, 1023)]
 
 
 def make(dtype, s, e, c, d, f, seed=0):
@@ -127,6 +130,17 @@ def test_large_tiles(dtype, case):
     m = make(dtype, *case, seed=2)
     check_forward(m, dtype, "cuda")
     check_backward(m, dtype, "cuda")
+
+
+@TYPES
+@pytest.mark.parametrize("case", LAST, ids=str)
+def test_shared_last_tiles(dtype, case):
+    m = make(dtype, *case, seed=4)
+    check_forward(m, dtype, "cuda")
+    check_backward(m, dtype, "cuda")
+    first = [*forward(m), *backward(m).values()]
+    for a, b in zip(first, [*forward(m), *backward(m).values()]):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
