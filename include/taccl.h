@@ -577,7 +577,9 @@ taccl_status_t taccl_combine_backward(const taccl_combine_backward_t *a, taccl_s
  * cols / 64, each rounded up. cols and hidden in whole 16-byte units and arrays on
  * 16 bytes are fastest. `workspace`: taccl_ffn_workspace(sources, E, capacity,
  * hidden, dtype, backward) bytes, 16-byte aligned, not shared with another call
- * in flight.
+ * in flight. Of them min(64 MB, 1.5 MB + 8192 a row of the buffer) are for the sums
+ * of tiles that several blocks share; min(64 MB, 768 KB + 64 a row) for these are
+ * enough, with fewer tiles shared and sums in another order.
  */
 typedef struct {
   int64_t capacity;

@@ -103,7 +103,7 @@ void check_ffn(Check &c, const A &a, bool backward) {
   c.array(a.w_in, size, "w_in");
   c.array(a.w_out, size, "w_out");
   c.workspace(a.workspace, a.workspace_bytes,
-              ffn_space(z.sources, z.experts, z.capacity, z.hidden, z.dtype, backward).bytes);
+              ffn_space(z.sources, z.experts, z.capacity, z.hidden, z.dtype, backward).least);
 }
 
 taccl_status_t launched(hipError_t e, const char *call) {

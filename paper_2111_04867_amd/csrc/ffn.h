@@ -27,8 +27,8 @@ struct FfnSpace {
   int64_t dpre;       // T [E][sources * capacity][2 hidden] (backward)
   int64_t done;       // int32 [4][kSplitTiles]: parts of a product's tiles that are there
   int64_t partial;    // float: their sums
-  int64_t partial_bytes;
-  int64_t bytes;
+  int64_t least;      // bytes that a call needs
+  int64_t bytes;      // and that it uses
 };
 constexpr int kSplitTiles = 1024;
 FfnSpace ffn_space(int64_t sources, int64_t experts, int64_t capacity, int64_t hidden, int dtype,

@@ -62,8 +62,8 @@ FfnSpace ffn_space(int64_t sources, int64_t experts, int64_t capacity, int64_t h
   s.partial = s.done + 4 * 4 * kSplitTiles;
   // parts are worth it where a product has few tiles, small ones, and weights'
   // gradients over many rows, or few in its last turn
-  s.partial_bytes = rounded(std::min<int64_t>(64 << 20, (3 << 18) + 4096 * rows));
-  s.bytes = s.partial + s.partial_bytes;
+  s.least = s.partial + rounded(std::min<int64_t>(64 << 20, (3 << 18) + 64 * rows));
+  s.bytes = s.partial + rounded(std::min<int64_t>(64 << 20, (3 << 19) + 8192 * rows));
   return s;
 }
 
@@ -699,14 +699,18 @@ struct Products {
     g.col_tiles = (int)((n + k.cols - 1) / k.cols);
     g.row_tiles = (int)((m + k.rows - 1) / k.rows);
     // Few tiles share their steps among parts, as many as CUs hold at two blocks
-    // each (one of the largest tiles), of at least eight steps (2 x 340 rows of 4587 f32, hidden 32: 64 us a
-    // call without, 27 with).
+    // each (one of the largest tiles), of at least eight steps (2 x 340 rows of 4587
+    // f32, hidden 32: 64 us a call without, 27 with). More sums than 4096
+    // bytes a row cost more than they save (gradient of 4 x 1000 rows of 2048 bf16,
+    // hidden 1024: 138 us, with 8192 142).
     const int64_t count = (int64_t)g.experts * g.row_tiles * g.col_tiles;
     const int64_t step = dtype == TACCL_F32 ? 32 : 64, size = (int64_t)k.rows * k.cols * 4;
+    const int64_t sums = std::min(partial_bytes, (3 << 18) + 4096 * base.experts * slots);
     int64_t parts = 1;
     if (count <= kSplitTiles)
-      parts = std::max<int64_t>(1, std::min({std::min(2, k.held()) * (int64_t)cus / count, K / (8 * step), (int64_t)16,
-                                             (partial_bytes - used) / (count * size)}));
+      parts = std::max<int64_t>(
+          1, std::min({std::min(2, k.held()) * (int64_t)cus / count, K / (8 * step), (int64_t)16,
+                       (sums - used) / (count * size)}));
     g.parts = (int)parts;
     g.done = done + number * kSplitTiles;
     g.partial = partial + used / 4;
@@ -723,19 +727,22 @@ struct Products {
     uint32_t blocks;
     int64_t used = 0;
     ProductArgs g = args(k, number, a, b, out, m, n, K, blocks, used);
-    // The tiles of rows that exist may leave most of the chip without one in its
+    // The tiles of rows that exist may leave most of the chip without one in their
     // last turn, which only the device knows: up to four blocks share such a tile,
-    // of at least eight steps each (us a call without and so: 8 x 600 rows of 2048
-    // f32, hidden 1024 654 and 554; 4 x 1030 bf16 105 and 102; gradient of 6 x 700
-    // bf16, hidden 1408 281 and 260, of 8 x 200 of 4096, hidden 1536 303 and 286).
-    // Through registers sixteen (20 x 500 rows of 2047 f16, hidden 1023: 247 us
-    // without, 263 with eight).
+    // of at least eight steps each, one block per CU in all (us a call without and
+    // so: 8 x 600 rows of 2048 f32, hidden 1024 654 and 556, 570 with two blocks per
+    // CU; 8 x 200 of 4096 bf16, hidden 1536, room for 1024 165 and 144; gradient of
+    // 6 x 700 of 2048 bf16, hidden 1408 277 and 253). Adding up the parts takes as
+    // long as about eight steps: axes of less than 24 are not shared (gradient of 4
+    // x 1000 of 2048 bf16, hidden 1024 132, shared 138). Through registers parts have
+    // sixteen (20 x 500 rows of 2047 f16, hidden 1023 247, with eight 263).
     const int64_t steps = K / (dtype == TACCL_F32 ? 32 : 64), round = (int64_t)cus * k.held();
-    const int64_t last_parts = std::min<int64_t>(steps / (fast ? 8 : 16), 4);
+    const int64_t last_parts =
+        steps < 24 ? 1 : std::min<int64_t>(steps / (fast ? 8 : 16), 4);
     if (g.parts == 1 && last_parts > 1 && round <= kSplitTiles && round % 256 == 0) {
       g.round = (uint32_t)round;
       g.last_parts = (uint32_t)last_parts;
-      g.room = (uint32_t)std::min(round, partial_bytes / ((int64_t)k.rows * k.cols * 4));
+      g.room = (uint32_t)std::min<int64_t>(cus, partial_bytes / ((int64_t)k.rows * k.cols * 4));
       blocks = (uint32_t)((blocks + round - 1) / round * round);
     }
     g.more = more;
@@ -766,7 +773,7 @@ Products products(const A &a, const FfnSpace &sp, bool fast, int cus, hipStream_
   for (int i = 0; i < kLists; i++) p.tiles[i] = (const FfnTile *)(ws + sp.tiles[i]);
   p.done = (int32_t *)(ws + sp.done);
   p.partial = (float *)(ws + sp.partial);
-  p.partial_bytes = sp.partial_bytes;
+  p.partial_bytes = std::min(a.workspace_bytes, sp.bytes) - sp.partial;
   return p;
 }
 

@@ -8,6 +8,7 @@ import torch
 
 import expert_forms as F
 from paper_2111_04867_amd import experts as X
+from paper_2111_04867_amd.binding import TacclError
 
 pytestmark = pytest.mark.gpu
 TYPES = pytest.mark.parametrize("dtype", F.TYPES.values(), ids=F.TYPES)
@@ -141,6 +142,22 @@ def test_shared_last_tiles(dtype, case):
     first = [*forward(m), *backward(m).values()]
     for a, b in zip(first, [*forward(m), *backward(m).values()]):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+@TYPES
+@pytest.mark.parametrize("case", [LONG[1], LAST[0], LAST[1]], ids=str)
+def test_the_least_workspace(dtype, case, monkeypatch):
+    """Of the sums' bytes the least that is taken: nothing is written behind it."""
+    m = make(dtype, *case, seed=5)
+    rows, full = case[0] * case[1] * case[2], X.ffn_workspace
+    less = min(64 << 20, (3 << 19) + 8192 * rows) - min(64 << 20, (3 << 18) + 64 * rows)
+    # both are rounded up to 256
+    monkeypatch.setattr(X, "ffn_workspace", lambda *a: full(*a) - (less - 256) // 256 * 256)
+    check_forward(m, dtype, "cuda")
+    check_backward(m, dtype, "cuda")
+    monkeypatch.setattr(X, "ffn_workspace", lambda *a: full(*a) - less - 512)
+    with pytest.raises(TacclError, match="workspace too small"):
+        forward(m)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
