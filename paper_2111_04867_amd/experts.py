@@ -366,11 +366,11 @@ def combine(buffer, experts, slots, counts, weights):
 
 class _FfnFn(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, buffer, counts, w_in, w_out):
+    def forward(ctx, buffer, counts, w_in, w_out, recorded):
         hidden = w_out.shape[2]
         out = torch.empty_like(buffer)
         pre = None
-        if any(ctx.needs_input_grad):
+        if recorded and any(ctx.needs_input_grad):
             pre = torch.empty(*buffer.shape[:-1], 2 * hidden, dtype=buffer.dtype,
                               device=buffer.device)
         ffn_tensors(buffer, counts, w_in, w_out, out,
@@ -389,12 +389,15 @@ class _FfnFn(torch.autograd.Function):
         ffn_backward_tensors(dout.contiguous(), buffer, counts, w_in, w_out, pre,
                              _workspace(size, buffer), dbuffer=given[0], dw_in=given[1],
                              dw_out=given[2])
-        return given[0], None, given[1], given[2]
+        return given[0], None, given[1], given[2], None
 
 
 def ffn(buffer, counts, w_in, w_out):
-    """Rows of ffn_tensors; gradients flow to the buffer and the weights."""
-    return _FfnFn.apply(buffer, counts, w_in, w_out)
+    """Rows of ffn_tensors; gradients flow to the buffer and the weights. What
+    they need is kept only where autograd records the call."""
+    # asked for here: within forward gradients are off, and needs_input_grad
+    # tells what the tensors want under no_grad too
+    return _FfnFn.apply(buffer, counts, w_in, w_out, torch.is_grad_enabled())
 
 
 class _FfnTokensFn(torch.autograd.Function):
