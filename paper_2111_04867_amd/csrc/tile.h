@@ -32,10 +32,15 @@ static __device__ Chunk zero_chunk;
 __device__ __forceinline__ void load_to_lds(const void *p, char *lds) {
   const uint32_t at = __builtin_amdgcn_readfirstlane(
       (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds);
+  // m0 is declared so that no move to it is carried past this one; that it is
+  // not kept for the code behind, which the compiler warns of, is meant.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                :
                : "v"(p), "s"(at)
-               : "memory");
+               : "memory", "m0");
+#pragma clang diagnostic pop
 }
 // All but the newest kLater of the wavefront's loads are there and its reads of
 // LDS are done, and the same holds for the block's other wavefronts.
