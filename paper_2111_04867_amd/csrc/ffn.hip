@@ -454,6 +454,7 @@ __device__ __forceinline__ void product(const ProductArgs &g, uint32_t b, char *
     const uint32_t tile = id - alone;
     constexpr int kAll = MI * NI, kOnce = kAll < 16 ? kAll : 16;
     float *sums = g.partial + (int64_t)tile * parts * (BM * BN) + wave * (kAll * 256) + lane * 4;
+    put_ready();
 #pragma unroll
     for (int i = 0; i < kAll; i++) put_chunk(sums + part * (BM * BN) + i * 256, acc[i / NI][i % NI]);
     if (!last_of(g.done + tile, (int)parts, (int32_t *)lds)) return;

@@ -68,9 +68,13 @@ __device__ __forceinline__ F4 get(const float *p) {
 }
 // The same for a tile: chunks of 64 lanes' 16 bytes, 1 KB apart, N of them on
 // their way at once (4 bytes at a time, as atomics: 32 tiles of 128 x 256 in four
-// parts each took 70 us longer)
+// parts each took 70 us longer). The compiler does not look into the assembly, so
+// its wait states are placed here: 12 behind a matrix instruction whose results are
+// put (put_ready, once for all of them) and 2 before a store's registers are
+// written again.
+__device__ __forceinline__ void put_ready() { asm volatile("s_nop 15" ::: "memory"); }
 __device__ __forceinline__ void put_chunk(float *p, F4 v) {
-  asm volatile("global_store_dwordx4 %0, %1, off sc1\n\ts_nop 0" : : "v"(p), "v"(v) : "memory");
+  asm volatile("global_store_dwordx4 %0, %1, off sc1\n\ts_nop 1" : : "v"(p), "v"(v) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void get_chunks(F4 (&v)[N], const float *p) {
