@@ -67,6 +67,9 @@ def test_memory_and_results_of_an_evaluation():
     with torch.no_grad():
         got = X.ffn(x, counts, w_in, w_out)
     used = torch.cuda.max_memory_allocated() - before
-    # the allocator rounds each of the two up to 512 bytes
-    assert used <= x.nbytes + X.ffn_workspace(x.shape, f, x.dtype) + 2 * 512
+    # the allocator rounds the two arrays up to 512 bytes each, and a block for the
+    # larger one keeps a rest of up to 1 MB; pre would take 4 * 300 * 2 * 2048 * 2
+    # bytes, 9.8 MB
+    rest = 2 * 512 + (1 << 20)
+    assert used <= x.nbytes + X.ffn_workspace(x.shape, f, x.dtype) + rest
     assert torch.equal(got, want)
