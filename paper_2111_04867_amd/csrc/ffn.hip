@@ -633,6 +633,25 @@ bool aligned16(P... p) {
   return (((uintptr_t)p % 16 == 0) && ...);
 }
 
+// Time of a step of 128 bytes by tile size: a CU holds `held` blocks, which take
+// `full` microseconds a step each, and `alone` if there is only one. Measured: f16
+// and bf16 with all CUs busy, on the up projection of 64 x 980 rows of 4096, hidden
+// 1536 (1434, 1571, 1773 and 2784 us from Large to Small), single blocks on 4 x 196
+// rows; in 32 bits the matrix instructions' time.
+struct Pace {
+  Size size;
+  int rows, cols, held;
+  double full, alone;
+};
+constexpr Pace kPaces16[] = {{kLarge, 256, 256, 1, 1.75, 1.75},
+                             {kWide, 128, 256, 1, 1.15, 1.1},
+                             {kMedium, 128, 128, 2, 1.3, 0.8},
+                             {kSmall, 64, 64, 4, 0.95, 0.5},
+                             {kTiny, 32, 64, 2, 0.45, 0.45}};
+constexpr Pace kPaces32[] = {{kMedium, 128, 128, 2, 3.4, 1.8},
+                             {kSmall, 64, 64, 4, 1.8, 0.6},
+                             {kTiny, 32, 64, 2, 0.6, 0.4}};
+
 // What the launches of a call share
 struct Products {
   ProductArgs base{};
@@ -649,28 +668,11 @@ struct Products {
     return base.experts * ((m + rows - 1) / rows) * ((n + cols - 1) / cols);
   }
   // Size of the tiles of a product of m rows and n columns per expert: the one
-  // whose steps take the least time. A CU holds `held` blocks, which take `full`
-  // microseconds for a step of 128 bytes each, and `alone` if there is only one.
-  // Measured: f16 and bf16 with all CUs busy, on 64 x 980 x 4096 x 3 Ki (1434,
-  // 1571, 1773 and 2784 us from Large to Small), single blocks on 4 x 196 rows;
-  // in 32 bits the matrix instructions' time.
+  // whose steps take the least time
   Size size_of(int64_t m, int64_t n) const {
-    struct Cost {
-      Size size;
-      int rows, cols, held;
-      double full, alone;
-    };
-    static constexpr Cost k16[] = {{kLarge, 256, 256, 1, 1.75, 1.75},
-                                   {kWide, 128, 256, 1, 1.15, 1.1},
-                                   {kMedium, 128, 128, 2, 1.3, 0.8},
-                                   {kSmall, 64, 64, 4, 0.95, 0.5},
-                                   {kTiny, 32, 64, 2, 0.45, 0.45}};
-    static constexpr Cost k32[] = {{kMedium, 128, 128, 2, 3.4, 1.8},
-                                   {kSmall, 64, 64, 4, 1.8, 0.6},
-                                   {kTiny, 32, 64, 2, 0.6, 0.4}};
     Size best = kMedium;
     double least = 1e300;
-    auto consider = [&](const Cost &c) {
+    auto consider = [&](const Pace &c) {
       if (!fast && c.size >= kWide) return;
       const double turns = (double)count(m, n, c.rows, c.cols) / (c.held * cus);
       const double t = std::max(c.alone, turns * c.full);
@@ -680,9 +682,9 @@ struct Products {
       }
     };
     if (dtype == TACCL_F32)
-      for (const Cost &c : k32) consider(c);
+      for (const Pace &c : kPaces32) consider(c);
     else
-      for (const Cost &c : k16) consider(c);
+      for (const Pace &c : kPaces16) consider(c);
     return best;
   }
 
@@ -847,15 +849,16 @@ hipError_t launch_ffn_backward(const taccl_ffn_backward_t &a, int cus, hipStream
   const bool each = fast && a.dtype != TACCL_F32 &&
                     std::min({p.size_of(p.slots, D), p.size_of(2 * F, D), p.size_of(D, F)}) >= kWide;
   // the longest tile alone, or all of them at full CUs
-  auto time = [&](int n, int held, double full, double alone) {
+  auto time = [&](Size of) {
+    const Pace *c = a.dtype == TACCL_F32 ? kPaces32 : kPaces16;
+    while (c->size != of) c++;
     const double step = a.dtype == TACCL_F32 ? 32 : 64, by_f = 2 * F / step, by_rows = p.slots / step;
-    const double all = p.count(p.slots, D, n, n) * by_f +
-                       (p.count(2 * F, D, n, n) + p.count(D, F, n, n)) * by_rows;
-    return std::max(alone * std::max(by_f, by_rows), all * full / (held * cus));
+    const double all = p.count(p.slots, D, c->rows, c->cols) * by_f +
+                       (p.count(2 * F, D, c->rows, c->cols) + p.count(D, F, c->rows, c->cols)) *
+                           by_rows;
+    return std::max(c->alone * std::max(by_f, by_rows), all * c->full / (c->held * cus));
   };
-  const bool medium = a.dtype == TACCL_F32 ? time(128, 2, 3.4, 1.8) < time(64, 4, 1.8, 0.6)
-                                           : time(128, 2, 1.3, 0.8) < time(64, 4, 0.95, 0.5);
-  const Size size = medium ? kMedium : kSmall;
+  const Size size = time(kMedium) < time(kSmall) ? kMedium : kSmall;
   const Kernel k = a.dtype == TACCL_F32    ? last_kernel<float>(mapped, fast, size)
                    : a.dtype == TACCL_BF16 ? last_kernel<bf16_t>(mapped, fast, size)
                                            : last_kernel<f16_t>(mapped, fast, size);
