@@ -579,7 +579,9 @@ taccl_status_t taccl_combine_backward(const taccl_combine_backward_t *a, taccl_s
  * hidden, dtype, backward) bytes, 16-byte aligned, not shared with another call
  * in flight. Of them min(64 MB, 1.5 MB + 8192 a row of the buffer) are for the sums
  * of tiles that several blocks share; min(64 MB, 768 KB + 64 a row) for these are
- * enough, with fewer tiles shared and sums in another order.
+ * enough, with fewer tiles shared and sums in another order. The same call gives
+ * the same bits; a row's last bits may differ with the other rows' counts, which
+ * decide where its sums begin and are cut.
  */
 typedef struct {
   int64_t capacity;
